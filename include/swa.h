@@ -56,11 +56,12 @@ typedef enum {
     SWA_ERR_UNSUPPORTED_D = -3,     /* d not in {64, 128} */
     SWA_ERR_UNSUPPORTED_DTYPE = -4, /* dtype not a swa_dtype, or a cache format the call does not take */
     SWA_ERR_BAD_SPARSITY = -5,      /* sparsity_bp outside 0..9999 */
-    SWA_ERR_CAPACITY = -6,          /* cap above SWA_MAX_CAP, or (status) a cache was full */
+    SWA_ERR_CAPACITY = -6,          /* cap above SWA_MAX_CAP, a pool too large, or (status) a cache was full or pages ran out */
     SWA_ERR_HIP = -7,               /* a HIP runtime call failed */
     SWA_ERR_ALIGNMENT = -8,         /* a row pointer is not 16-byte aligned */
     SWA_ERR_HOST_STORE_FULL = -9,   /* (status) a pair's host store had no room for its evicted tokens */
-    SWA_ERR_BAD_REQUEST = -10       /* (status) a reload named a token that the host store does not hold */
+    SWA_ERR_BAD_REQUEST = -10       /* (status) a reload named a token that the host store does not hold, or a page or slot
+                                       lies outside the pool */
 } swa_status;
 
 typedef struct {
@@ -432,6 +433,127 @@ int swa_reload_tokens(const swa_params *params, const swa_host_store *store, con
                       const int32_t *req_cnt, int32_t max_req, void *k_cache, void *v_cache,
                       float *score, int32_t *pos, const int32_t *cache_len, int32_t *new_len,
                       void *workspace, void *stream);
+
+/*
+ * Paged cache, for layers whose cache is not sparsified and for contexts beyond SWA_MAX_CAP: keys and values live in a pool
+ * of pages of page_size tokens, a table names each sequence's pages, and key/value heads may be shared by several query heads.
+ * Three calls make a step: swa_paged_plan finds room for the new tokens, swa_paged_append (once a layer) writes their rows,
+ * swa_paged_decode (once a layer) attends over the cache.  Conventions as above, and
+ *   - tensors:
+ *       k_pages, v_pages  [n_pages, h_kv, page_size, d]  dtype, or int8 codes with SWA_KV_INT8
+ *       k_scale, v_scale  [n_pages, h_kv, page_size]     float32, with SWA_KV_INT8 only (NULL otherwise): a row's value is
+ *                                                        its code times its scale
+ *       block_table       [b, max_pages] int32           page of tokens j*page_size ... of a sequence
+ *       cache_len         [b] int32
+ *     Token t of sequence s sits in slot block_table[s][t / page_size] * page_size + t % page_size, at offset t % page_size of that page.
+ *     A pool with one page for each sequence (page_size = cap, block_table[s][0] = s) is a cache [b, h, cap, d] as the other
+ *     calls take it, and one with pages of one token is an array of rows [n, h, d], such as their k_new and v_new.
+ *   - A negative cache_len marks an unused row of a padded batch.
+ *   - Lists that grow by a call go through two arrays (cache_len and new_len, free_state and free_state_out), which the caller
+ *     passes swapped on the next call, as with SWA_FUSE_COMPACTION: calls can be captured, and made again on the same arguments.
+ *   - Device-side conditions set sticky bits in the workspace (swa_paged_check_status): SWA_ERR_CAPACITY and SWA_ERR_BAD_REQUEST
+ *     where a call says so.  No page or slot outside the pool is read or written.
+ */
+#define SWA_MAX_PAGED_SEQS 4096
+#define SWA_MAX_ROPE_AXES 4
+
+/* swa_paged_params.flags: SWA_KV_INT8 (dtype SWA_F16 or SWA_BF16) and this bit: a rotated pair of channels is (2i, 2i+1)
+ * instead of (i, i + rot_dim/2). */
+#define SWA_ROPE_INTERLEAVED 32
+
+typedef struct {
+    int32_t b;          /* sequences, 1..SWA_MAX_PAGED_SEQS */
+    int32_t h_q;        /* query heads, a multiple of h_kv; query head i reads key/value head i / (h_q / h_kv) */
+    int32_t h_kv;       /* key/value heads */
+    int32_t d;          /* head dimension, 64 or 128 */
+    int32_t page_size;  /* tokens in a page, 1..SWA_MAX_CAP */
+    int32_t n_pages;    /* pages in the pool; n_pages * h_kv * page_size < 2^31 */
+    int32_t max_pages;  /* width of the block table; max_pages * page_size < 2^31 */
+    int32_t dtype;      /* swa_dtype of q, k, v, weights, out, and of the pages without SWA_KV_INT8 */
+    float scale;        /* logit scale; 0 selects 1/sqrt(d) */
+    int32_t window;     /* 0, or how many of the last tokens the attention sees */
+    int32_t len_bound;  /* 0, or an upper bound on cache_len for swa_paged_decode, which it sizes its launch to */
+    int32_t flags;
+    int32_t rot_dim;    /* channels that the rotation takes, the first ones of a row: a multiple of 16, 0..d */
+    int32_t axes;       /* position axes, 1..SWA_MAX_ROPE_AXES */
+    int32_t section[SWA_MAX_ROPE_AXES]; /* channel pairs of each axis, in order; their sum is rot_dim/2 */
+    float eps;          /* of the norm, >= 0 */
+} swa_paged_params;
+
+/* Rows [n, heads, d] of which each is dense, `stride` elements apart (at least heads * d, with 16-byte alignment of every row):
+ * a tensor of its own, or one operand's part of a fused projection. */
+typedef struct {
+    const void *data;
+    int64_t stride;
+} swa_rows;
+
+/* Workspace of the paged calls, as swa_workspace_bytes, swa_workspace_init and swa_check_status are for the others.  The size
+ * goes by b, the heads and d.  Calls that overlap in time need workspaces of their own. */
+size_t swa_paged_workspace_bytes(const swa_paged_params *params);
+int swa_paged_workspace_init(const swa_paged_params *params, void *workspace, void *stream);
+int swa_paged_check_status(const swa_paged_params *params, void *workspace, void *stream, int32_t *status_out);
+
+/*
+ * Block tables, slots and positions for the tokens that sequences bring (new_cnt[s] of them each), on the GPU.
+ * The free pages are a ring: free_ring[(head + i) mod n_pages], i < count, with (head, count) in free_state.  A sequence with a
+ * negative cache_len gets nothing.
+ *   1. rows: the call's new tokens are packed, sequence after sequence; row_start[s] = sum of max(new_cnt, 0) before s,
+ *      row_start[b] the sum of all (saturated at 2^30).
+ *   2. pages: sequence s needs the pages from ceil(cache_len / page_size) to ceil((cache_len + new_cnt) / page_size); they come
+ *      from the ring's head in the order of sequences and pages, and their numbers go to block_table.
+ *   3. a sequence is refused as a whole where cache_len + new_cnt exceeds max_pages * page_size, its rows end beyond
+ *      max_rows, or the free pages end before its own (what refused sequences asked for is not handed on within the call):
+ *      new_len = cache_len, slots -1, and the SWA_ERR_CAPACITY bit is set.
+ *   4. slot[r], pos[r] for r < max_rows: the row's slot, and its position in its sequence; -1 and 0 for rows of refused
+ *      sequences and behind the last one.  new_len[s] = cache_len[s] + new_cnt[s].
+ *   5. new_cnt[s] < 0: the sequence has finished.  Its pages go to the ring's end (in the order of sequences and pages, for
+ *      the next call), new_len[s] = 0.
+ * A cache_len above max_pages * page_size, and a page number outside the pool in the ring or in a finished sequence's row, set
+ * the SWA_ERR_BAD_REQUEST bit; such a sequence is left alone, such a page gets slot -1.
+ *   new_cnt, cache_len [b] (in); new_len [b], row_start [b+1], slot, pos [max_rows], free_state_out [2] (out);
+ *   block_table, free_ring [n_pages] (in/out); free_state [2] (in); 1 <= max_rows <= 2^24.
+ */
+int swa_paged_plan(const swa_paged_params *params, const int32_t *new_cnt, const int32_t *cache_len, int32_t *new_len,
+                   int32_t *block_table, int32_t *free_ring, const int32_t *free_state, int32_t *free_state_out,
+                   int32_t max_rows, int32_t *row_start, int32_t *slot, int32_t *pos, void *workspace, void *stream);
+
+/*
+ * Queries, keys and values of new rows on their way into the cache, in one pass over them.  For every row r < n_rows with
+ * slot[r] >= 0 and every head:
+ *   norm      x_i <- x_i / sqrt(mean_j x_j^2 + eps) * weight_i       (queries where q_weight is given, keys where k_weight is)
+ *   rotation  (x_i, x_j) <- (x_i cos a - x_j sin a, x_j cos a + x_i sin a) for the pairs of the first rot_dim channels, with the
+ *             angle a = pos[axis of the pair][r] * inv_freq[pair]    (queries and keys)
+ * q_out gets the queries, slot[r] of k_pages and v_pages the keys and the values as they came.  All in fp32, the angle in
+ * fp64 until it is reduced to one turn; rounded once.  With SWA_KV_INT8 a row is stored as scale = max |x| / 127 and codes
+ * round(x / scale), ties to even (zeros where scale is below 2^-126); a row with a value that is not finite reads back as NaN.
+ * A row with a negative slot is left out: nothing is read or written for it.  A slot outside the pool is left out too and
+ * sets the SWA_ERR_BAD_REQUEST bit.  The slots of one call are distinct (as swa_paged_plan makes them): of two rows with the
+ * same slot either may end up in it, or some heads of each.
+ *   q [n_rows, h_q, d], k, v [n_rows, h_kv, d] (in); pos [axes, n_rows] int32; slot [n_rows]; inv_freq [rot_dim/2] float32
+ *   (pos and inv_freq may be NULL when rot_dim == 0); q_weight, k_weight [d] dtype or NULL; q_out [n_rows, h_q, d] dense (out),
+ *   which may be q itself where that is dense; k_pages, v_pages, k_scale, v_scale (out).
+ */
+int swa_paged_append(const swa_paged_params *params, swa_rows q, swa_rows k, swa_rows v, int32_t n_rows, const int32_t *pos,
+                     const int32_t *slot, const float *inv_freq, const void *q_weight, const void *k_weight, void *q_out,
+                     void *k_pages, void *v_pages, float *k_scale, float *v_scale, void *workspace, void *stream);
+
+/*
+ * Attention of the newest token of every sequence over its pages (Eq. 1 over all cached tokens, or the last `window`):
+ *   out[r] = sum_t softmax_t(q[r] . K[t] * scale) V[t],  lse[r] = log sum_t exp(q[r] . K[t] * scale)
+ * for t in [max(0, cache_len[s] - window), cache_len[s]) and r the sequence's row: s itself, or with row_start (as
+ * swa_paged_plan writes it) the last of rows row_start[s] .. row_start[s+1] - 1.  Sequences with a negative cache_len, without
+ * rows, or with a row beyond n_rows are skipped: nothing is written for them.  Where no token is left or every logit is -inf (so
+ * for cache_len = 0), out = 0 and lse = -inf.
+ * Accumulated in fp32; the weights are rounded to dtype (8-bit codes: to 16 bits of mantissa) for their product with the
+ * values, out is rounded once.  A call's results do not depend on the order in which its workgroups run.
+ * A sequence longer than max_pages * page_size or a stated len_bound is skipped, and the SWA_ERR_CAPACITY bit is set.  Tokens of
+ * pages outside the pool are left out of the sums, and the SWA_ERR_BAD_REQUEST bit is set.
+ *   q [n_rows, h_q, d] (in); row_start [b+1] or NULL (then n_rows >= b); out [n_rows, h_q, d] dense, lse [n_rows, h_q] float32 or
+ *   NULL (out).
+ */
+int swa_paged_decode(const swa_paged_params *params, swa_rows q, int32_t n_rows, const int32_t *row_start, const void *k_pages,
+                     const void *v_pages, const float *k_scale, const float *v_scale, const int32_t *block_table,
+                     const int32_t *cache_len, void *out, float *lse, void *workspace, void *stream);
 
 /*
  * Measurement aid, not part of the method: reads `bytes` (rounded down to a multiple of 104 KiB)

@@ -35,12 +35,16 @@ SWA_KV_INT8 = 8
 SWA_SPLIT_ROWS = 16
 SWA_MAX_WINDOW_ROWS = 64
 SWA_STATIC_SCRATCH_BYTES = 8 << 20
+SWA_MAX_PAGED_SEQS = 4096
+SWA_MAX_ROPE_AXES = 4
+SWA_ROPE_INTERLEAVED = 32
 
 DTYPE_CODE = {torch.float32: SWA_F32, torch.float16: SWA_F16, torch.bfloat16: SWA_BF16}
 EXPORTS = ["swa_strerror", "swa_workspace_bytes", "swa_workspace_init", "swa_check_status",
            "swa_budget", "swa_prefill_scores", "swa_decode_step", "swa_compact_kv", "swa_quantize_kv",
            "swa_decode_step_q8", "swa_prefill_rows", "swa_decode_step_window", "swa_prefill_attention", "swa_probe_stream_read",
-           "swa_prepare", "swa_decode_step_static", "swa_decode_step_window_q8", "swa_offload_evicted", "swa_reload_tokens"]
+           "swa_prepare", "swa_decode_step_static", "swa_decode_step_window_q8", "swa_offload_evicted", "swa_reload_tokens",
+           "swa_paged_workspace_bytes", "swa_paged_workspace_init", "swa_paged_check_status", "swa_paged_plan", "swa_paged_append", "swa_paged_decode"]
 
 
 class SwaParams(ctypes.Structure):
@@ -55,6 +59,18 @@ class SwaHostStore(ctypes.Structure):
                 ("pos", ctypes.c_void_p), ("len", ctypes.c_void_p), ("host_cap", ctypes.c_int32)]
 
 
+class SwaPagedParams(ctypes.Structure):
+    _fields_ = [("b", ctypes.c_int32), ("h_q", ctypes.c_int32), ("h_kv", ctypes.c_int32), ("d", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("window", ctypes.c_int32),
+                ("len_bound", ctypes.c_int32), ("flags", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("axes", ctypes.c_int32), ("section", ctypes.c_int32 * SWA_MAX_ROPE_AXES), ("eps", ctypes.c_float)]
+
+
+class SwaRows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+
+
 class SwaError(RuntimeError):
     def __init__(self, code: int, what: str):
         self.code = code
@@ -67,7 +83,8 @@ _native = None      # the native half (csrc/swa_native.cpp), bound to the entry 
 # Entry points whose arguments the native half converts: fn(params, arguments..., stream) -> status, or None where an argument is
 # not a plain tensor, an integer or None; the call then takes the general path below, with its errors.
 NATIVE = ("swa_decode_step", "swa_decode_step_q8", "swa_decode_step_window", "swa_decode_step_window_q8", "swa_decode_step_static",
-          "swa_compact_kv", "swa_prefill_scores", "swa_prefill_rows", "swa_prefill_attention", "swa_quantize_kv")
+          "swa_compact_kv", "swa_prefill_scores", "swa_prefill_rows", "swa_prefill_attention", "swa_quantize_kv",
+          "swa_paged_plan", "swa_paged_append", "swa_paged_decode")
 
 
 class _General:
@@ -86,7 +103,7 @@ def _native_half(L):
         warnings.warn(f"calls convert their arguments in Python, a few microseconds each: {e} "
                       "(`python -m paper_2403_17312_amd.build` builds the native half)")
         return _General()
-    N.bind({n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in NATIVE}, SwaParams)
+    N.bind({n: ctypes.cast(getattr(L, n), ctypes.c_void_p).value for n in NATIVE}, SwaParams, SwaPagedParams)
     return N
 
 
@@ -139,6 +156,19 @@ def lib():
         L.swa_prefill_attention.argtypes = [pp, vp, vp, vp, i32p, vp, ctypes.c_int32, vp, vp, vp]
         L.swa_probe_stream_read.restype = ctypes.c_int
         L.swa_probe_stream_read.argtypes = [vp, ctypes.c_size_t, vp, vp]
+        gp = ctypes.POINTER(SwaPagedParams)
+        L.swa_paged_workspace_bytes.restype = ctypes.c_size_t
+        L.swa_paged_workspace_bytes.argtypes = [gp]
+        L.swa_paged_workspace_init.restype = ctypes.c_int
+        L.swa_paged_workspace_init.argtypes = [gp, vp, vp]
+        L.swa_paged_check_status.restype = ctypes.c_int
+        L.swa_paged_check_status.argtypes = [gp, vp, vp, ctypes.POINTER(ctypes.c_int32)]
+        L.swa_paged_plan.restype = ctypes.c_int
+        L.swa_paged_plan.argtypes = [gp] + [vp] * 7 + [ctypes.c_int32] + [vp] * 5
+        L.swa_paged_append.restype = ctypes.c_int
+        L.swa_paged_append.argtypes = [gp] + [SwaRows] * 3 + [ctypes.c_int32] + [vp] * 12
+        L.swa_paged_decode.restype = ctypes.c_int
+        L.swa_paged_decode.argtypes = [gp, SwaRows, ctypes.c_int32] + [vp] * 11
         _lib, _native = L, _native_half(L)
     return _lib
 
@@ -355,6 +385,160 @@ def swa_compact_kv(params: SwaParams, k_cache, v_cache, score, pos, kept_idx, ke
             _ptr(kept_cnt), _ptr(cache_len), _ptr(workspace), _stream(stream))
     if rc != SWA_OK:
         raise SwaError(rc, "swa_compact_kv")
+
+
+def make_paged_params(b: int, h_q: int, h_kv: int, d: int, page_size: int, n_pages: int, max_pages: int, dtype, scale: float = 0.0,
+                      window: int = 0, len_bound: int = 0, flags: int = 0, rot_dim: int = 0, sections=None,
+                      eps: float = 0.0) -> SwaPagedParams:
+    """sections: rotated channel pairs of each position axis (None: one axis has all of them)."""
+    code = DTYPE_CODE[dtype] if isinstance(dtype, torch.dtype) else int(dtype)
+    parts = [rot_dim // 2] if sections is None else [int(n) for n in sections]
+    if not 1 <= len(parts) <= SWA_MAX_ROPE_AXES:
+        raise SwaError(SWA_ERR_BAD_SHAPE, "make_paged_params")
+    return SwaPagedParams(b, h_q, h_kv, d, page_size, n_pages, max_pages, code, scale, window, len_bound, flags, rot_dim, len(parts),
+                          (ctypes.c_int32 * SWA_MAX_ROPE_AXES)(*parts), eps)
+
+
+def _here(t: torch.Tensor) -> None:
+    if t.device.type != "cuda" or t.device.index != torch.cuda.current_device():
+        raise ValueError("tensors of a paged cache must be on the current GPU")
+
+
+def _gpu_ptr(t: Optional[torch.Tensor]):
+    ptr = _ptr(t)
+    if t is not None:
+        _here(t)
+    return ptr
+
+
+def _rows(t: torch.Tensor) -> SwaRows:
+    n, heads, d = t.shape
+    if t.stride(2) != 1 or (heads > 1 and t.stride(1) != d):
+        raise ValueError("the rows of q, k and v must be dense: [rows, heads, d] with a stride between rows only")
+    _here(t)
+    return SwaRows(t.data_ptr(), t.stride(0) if n > 1 else heads * d)
+
+
+def swa_paged_workspace_bytes(params: SwaPagedParams) -> int:
+    return int(lib().swa_paged_workspace_bytes(ctypes.byref(params)))
+
+
+def swa_paged_workspace_init(params: SwaPagedParams, workspace: torch.Tensor, stream=None) -> None:
+    _check(lib().swa_paged_workspace_init(ctypes.byref(params), _gpu_ptr(workspace), _stream(stream)), "swa_paged_workspace_init")
+
+
+def swa_paged_check_status(params: SwaPagedParams, workspace: torch.Tensor, stream=None) -> int:
+    st = ctypes.c_int32(0)
+    _check(lib().swa_paged_check_status(ctypes.byref(params), _gpu_ptr(workspace), _stream(stream), ctypes.byref(st)),
+           "swa_paged_check_status")
+    return st.value
+
+
+def swa_paged_plan(params: SwaPagedParams, new_cnt, cache_len, new_len, block_table, free_ring, free_state, free_state_out, max_rows: int,
+                   row_start, slot, pos, workspace, stream=None) -> None:
+    rc = _fast().swa_paged_plan(params, new_cnt, cache_len, new_len, block_table, free_ring, free_state, free_state_out, max_rows,
+        row_start, slot, pos, workspace, stream)
+    if rc is None:
+        rc = lib().swa_paged_plan(ctypes.byref(params), _gpu_ptr(new_cnt), _gpu_ptr(cache_len), _gpu_ptr(new_len), _gpu_ptr(block_table),
+            _gpu_ptr(free_ring), _gpu_ptr(free_state), _gpu_ptr(free_state_out), int(max_rows), _gpu_ptr(row_start), _gpu_ptr(slot),
+            _gpu_ptr(pos), _gpu_ptr(workspace), _stream(stream))
+    if rc != SWA_OK:
+        raise SwaError(rc, "swa_paged_plan")
+
+
+def swa_paged_append(params: SwaPagedParams, q, k, v, n_rows: int, pos, slot, inv_freq, q_weight, k_weight, q_out, k_pages, v_pages,
+                     k_scale, v_scale, workspace, stream=None) -> None:
+    rc = _fast().swa_paged_append(params, q, k, v, n_rows, pos, slot, inv_freq, q_weight, k_weight, q_out, k_pages, v_pages, k_scale,
+        v_scale, workspace, stream)
+    if rc is None:
+        rc = lib().swa_paged_append(ctypes.byref(params), _rows(q), _rows(k), _rows(v), int(n_rows), _gpu_ptr(pos), _gpu_ptr(slot),
+            _gpu_ptr(inv_freq), _gpu_ptr(q_weight), _gpu_ptr(k_weight), _gpu_ptr(q_out), _gpu_ptr(k_pages), _gpu_ptr(v_pages),
+            _gpu_ptr(k_scale), _gpu_ptr(v_scale), _gpu_ptr(workspace), _stream(stream))
+    if rc != SWA_OK:
+        raise SwaError(rc, "swa_paged_append")
+
+
+def swa_paged_decode(params: SwaPagedParams, q, n_rows: int, row_start, k_pages, v_pages, k_scale, v_scale, block_table, cache_len, out, lse,
+                     workspace, stream=None) -> None:
+    rc = _fast().swa_paged_decode(params, q, n_rows, row_start, k_pages, v_pages, k_scale, v_scale, block_table, cache_len, out, lse,
+        workspace, stream)
+    if rc is None:
+        rc = lib().swa_paged_decode(ctypes.byref(params), _rows(q), int(n_rows), _gpu_ptr(row_start), _gpu_ptr(k_pages),
+            _gpu_ptr(v_pages), _gpu_ptr(k_scale), _gpu_ptr(v_scale), _gpu_ptr(block_table), _gpu_ptr(cache_len), _gpu_ptr(out),
+            _gpu_ptr(lse), _gpu_ptr(workspace), _stream(stream))
+    if rc != SWA_OK:
+        raise SwaError(rc, "swa_paged_decode")
+
+
+class PagedCache:
+    """Device tensors of a paged cache: one pool per layer, one plan for all of them (allocation plumbing, and checks of what is
+    handed in).  A step is plan(), then append() and decode() for every layer."""
+
+    def __init__(self, params: SwaPagedParams, layers: int = 1, device="cuda"):
+        p = self.params = params
+        nbytes = swa_paged_workspace_bytes(p)
+        if not nbytes:
+            raise ValueError("no paged cache has these parameters")
+        self.dtype = {v: k for k, v in DTYPE_CODE.items()}[p.dtype]
+        int8 = bool(p.flags & SWA_KV_INT8)
+        shape = (p.n_pages, p.h_kv, p.page_size, p.d)
+
+        def pools(shape, dtype):
+            return [torch.zeros(shape, dtype=dtype, device=device) for _ in range(layers)]
+        self.k_pages, self.v_pages = (pools(shape, torch.int8 if int8 else self.dtype) for _ in "kv")
+        self.k_scale, self.v_scale = (pools(shape[:3], torch.float32) if int8 else [None] * layers for _ in "kv")
+        self.block_table = torch.full((p.b, p.max_pages), -1, dtype=torch.int32, device=device)
+        self.cache_len, self._other_len = (torch.zeros((p.b,), dtype=torch.int32, device=device) for _ in range(2))
+        self.free_ring = torch.arange(p.n_pages, dtype=torch.int32, device=device)
+        self.free_state = torch.tensor([0, p.n_pages], dtype=torch.int32, device=device)
+        self._other_state = torch.zeros_like(self.free_state)
+        self.row_start = torch.zeros((p.b + 1,), dtype=torch.int32, device=device)
+        self.workspace = torch.zeros((nbytes,), dtype=torch.uint8, device=device)
+        swa_paged_workspace_init(p, self.workspace)
+
+    def _expect(self, name, t, shape, dtype) -> None:
+        if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
+            raise ValueError(f"{name} must be {list(shape)} of {dtype}, this is {list(t.shape)} of {t.dtype}")
+
+    def plan(self, new_cnt, slot, pos, stream=None) -> None:
+        """new_cnt [b] (-1: finished); slot and pos [rows] are filled.  cache_len counts the new tokens afterwards."""
+        self._expect("new_cnt", new_cnt, (self.params.b,), torch.int32)
+        self._expect("slot", slot, (slot.numel(),), torch.int32)
+        self._expect("pos", pos, slot.shape, torch.int32)
+        swa_paged_plan(self.params, new_cnt, self.cache_len, self._other_len, self.block_table, self.free_ring, self.free_state,
+                       self._other_state, slot.numel(), self.row_start, slot, pos, self.workspace, stream)
+        self.cache_len, self._other_len = self._other_len, self.cache_len
+        self.free_state, self._other_state = self._other_state, self.free_state
+
+    def append(self, layer: int, q, k, v, slot, pos, inv_freq, q_out, q_weight=None, k_weight=None, stream=None) -> None:
+        """pos [rows], or [axes, rows] with several axes."""
+        p, n = self.params, q.shape[0]
+        self._expect("q", q, (n, p.h_q, p.d), self.dtype)
+        self._expect("k", k, (n, p.h_kv, p.d), self.dtype)
+        self._expect("v", v, (n, p.h_kv, p.d), self.dtype)
+        self._expect("q_out", q_out, (n, p.h_q, p.d), self.dtype)
+        self._expect("slot", slot, (n,), torch.int32)
+        if p.rot_dim:
+            self._expect("pos", pos, (p.axes, n) if pos.dim() > 1 or p.axes > 1 else (n,), torch.int32)
+            self._expect("inv_freq", inv_freq, (p.rot_dim // 2,), torch.float32)
+        for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+            if w is not None:
+                self._expect(name, w, (p.d,), self.dtype)
+        swa_paged_append(p, q, k, v, n, pos, slot, inv_freq, q_weight, k_weight, q_out, self.k_pages[layer], self.v_pages[layer],
+                         self.k_scale[layer], self.v_scale[layer], self.workspace, stream)
+
+    def decode(self, layer: int, q, out, lse=None, by_rows: bool = False, stream=None) -> None:
+        """by_rows: q and out hold the plan's packed rows, and each sequence's last one is meant; otherwise row s is sequence s."""
+        p, n = self.params, q.shape[0]
+        self._expect("q", q, (n, p.h_q, p.d), self.dtype)
+        self._expect("out", out, (n, p.h_q, p.d), self.dtype)
+        if lse is not None:
+            self._expect("lse", lse, (n, p.h_q), torch.float32)
+        swa_paged_decode(p, q, n, self.row_start if by_rows else None, self.k_pages[layer], self.v_pages[layer], self.k_scale[layer],
+                         self.v_scale[layer], self.block_table, self.cache_len, out, lse, self.workspace, stream)
+
+    def check_status(self, stream=None) -> int:
+        return swa_paged_check_status(self.params, self.workspace, stream)
 
 
 class DecodeState:

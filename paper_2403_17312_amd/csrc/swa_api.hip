@@ -249,15 +249,15 @@ const char* swa_strerror(int code)
     switch (code) {
         case SWA_OK: return "ok";
         case SWA_ERR_NULL: return "a required pointer is NULL";
-        case SWA_ERR_BAD_SHAPE: return "b, h, cap, w, scale or R out of range";
+        case SWA_ERR_BAD_SHAPE: return "b, h, cap, w, scale, R or another size out of range";
         case SWA_ERR_UNSUPPORTED_D: return "head dimension must be 64 or 128";
         case SWA_ERR_UNSUPPORTED_DTYPE: return "dtype must be SWA_F32, SWA_F16 or SWA_BF16";
         case SWA_ERR_BAD_SPARSITY: return "sparsity_bp must be in 0..9999";
-        case SWA_ERR_CAPACITY: return "cap exceeds SWA_MAX_CAP, or a sequence's cache was full";
+        case SWA_ERR_CAPACITY: return "cap exceeds SWA_MAX_CAP, a pool is too large, a sequence's cache was full, or pages ran out";
         case SWA_ERR_HIP: return "a HIP runtime call failed";
         case SWA_ERR_ALIGNMENT: return "tensor pointers must be 16-byte aligned";
         case SWA_ERR_HOST_STORE_FULL: return "a host store had no room for the evicted tokens";
-        case SWA_ERR_BAD_REQUEST: return "a reload named a token that the host store does not hold";
+        case SWA_ERR_BAD_REQUEST: return "a reload named a token that the host store does not hold, or a page or slot lies outside the pool";
         default: return "unknown swa_status";
     }
 }

@@ -5,6 +5,7 @@
 // What it saves is the host's time per call, which bounds small steps: 32 calls of about sixteen tensors each, on four short
 // pairs, 254 -> 198 us; 32 calls on 512 pairs 305 -> 292, where the GPU is the bound again.
 #include <Python.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -19,10 +20,12 @@ namespace {
 
 enum class Arg { ok, other, failed };
 
-PyObject* params_type = nullptr;                         // binding.py's SwaParams
+// binding.py's SwaParams, SwaPagedParams
+template <typename P>
+PyObject* params_type = nullptr;
 
-// A pointer argument: None, or a plain contiguous tensor.
-Arg pointer(PyObject* o, void*& out)
+// A pointer argument: None, or a plain contiguous tensor.  device: the one it has to be on (-1: not looked at).
+Arg pointer(PyObject* o, int device, void*& out)
 {
     if (o == Py_None) {
         out = nullptr;
@@ -31,7 +34,21 @@ Arg pointer(PyObject* o, void*& out)
     if (!THPVariable_CheckExact(o)) return Arg::other;
     const at::Tensor& t = THPVariable_Unpack(o);
     if (!t.is_contiguous()) return Arg::other;           // (refused on the general path)
+    if (device >= 0 && !(t.is_cuda() && t.device().index() == device)) return Arg::other;
     out = t.data_ptr();
+    return Arg::ok;
+}
+
+// Rows [n, heads, d] of which each is dense.
+Arg rows(PyObject* o, int device, swa_rows& out)
+{
+    if (!THPVariable_CheckExact(o)) return Arg::other;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (t.dim() != 3 || !(t.is_cuda() && t.device().index() == device)) return Arg::other;
+    const int64_t n = t.size(0), heads = t.size(1), d = t.size(2);
+    if (t.stride(2) != 1 || (heads > 1 && t.stride(1) != d)) return Arg::other;
+    out.data = t.data_ptr();
+    out.stride = n > 1 ? t.stride(0) : heads * d;
     return Arg::ok;
 }
 
@@ -48,11 +65,13 @@ Arg integer(PyObject* o, int64_t& out)
 
 // One argument of the C function, by its type there.
 template <typename A>
-Arg convert(PyObject* o, A& out)
+Arg convert(PyObject* o, int device, A& out)
 {
-    if constexpr (std::is_pointer_v<A>) {
+    if constexpr (std::is_same_v<A, swa_rows>) {
+        return rows(o, device, out);
+    } else if constexpr (std::is_pointer_v<A>) {
         void* p = nullptr;
-        const Arg r = pointer(o, p);
+        const Arg r = pointer(o, device, p);
         out = static_cast<A>(p);
         return r;
     } else {
@@ -68,16 +87,18 @@ Arg convert(PyObject* o, A& out)
 template <typename F>
 struct Entry;
 
-template <typename... A>
-struct Entry<int (*)(const swa_params*, A...)> {
+template <typename P, typename... A>
+struct Entry<int (*)(const P*, A...)> {
     static constexpr size_t N = sizeof...(A);            // the stream is the last one
+    static constexpr bool on_device = std::is_same_v<P, swa_paged_params>;   // the paged calls' tensors are on the current GPU
 
     // The arguments, or false where the general path has to look at them.
     template <size_t... I>
-    static bool convert_all(PyObject* const* args, swa_params& p, std::tuple<A...>& a, std::index_sequence<I...>)
+    static bool convert_all(PyObject* const* args, P& p, std::tuple<A...>& a, std::index_sequence<I...>)
     {
         Arg r = Arg::ok;
-        ((I + 1 < N && r == Arg::ok ? (void)(r = convert(args[1 + I], std::get<I>(a))) : (void)0), ...);
+        const int device = on_device ? (int)c10::hip::current_device() : -1;
+        ((I + 1 < N && r == Arg::ok ? (void)(r = convert(args[1 + I], device, std::get<I>(a))) : (void)0), ...);
         if (r != Arg::ok) return false;
         if (args[N] == Py_None) {
             std::get<N - 1>(a) = reinterpret_cast<void*>(c10::hip::getCurrentHIPStream().stream());
@@ -86,21 +107,21 @@ struct Entry<int (*)(const swa_params*, A...)> {
             std::get<N - 1>(a) = PyLong_AsVoidPtr(args[N]);
             if (PyErr_Occurred()) return false;
         }
-        if (reinterpret_cast<PyObject*>(Py_TYPE(args[0])) != params_type) return false;
+        if (reinterpret_cast<PyObject*>(Py_TYPE(args[0])) != params_type<P>) return false;
         Py_buffer params;
         if (PyObject_GetBuffer(args[0], &params, PyBUF_SIMPLE) != 0) return false;
-        const bool fits = params.len == (Py_ssize_t)sizeof(swa_params);
-        if (fits) p = *static_cast<const swa_params*>(params.buf);
+        const bool fits = params.len == (Py_ssize_t)sizeof(P);
+        if (fits) p = *static_cast<const P*>(params.buf);
         PyBuffer_Release(&params);
         return fits;
     }
 
     // Without the interpreter's lock.  An exception that leaves the library ends the process here, as it does by way of ctypes: caught
     // further out it would find the lock released and the call made a second time.
-    static int make(void* fn, const swa_params& p, const std::tuple<A...>& a) noexcept
+    static int make(void* fn, const P& p, const std::tuple<A...>& a) noexcept
     {
         PyThreadState* const held = PyEval_SaveThread();
-        const int rc = std::apply([&](A... v) { return reinterpret_cast<int (*)(const swa_params*, A...)>(fn)(&p, v...); }, a);
+        const int rc = std::apply([&](A... v) { return reinterpret_cast<int (*)(const P*, A...)>(fn)(&p, v...); }, a);
         PyEval_RestoreThread(held);
         return rc;
     }
@@ -109,7 +130,7 @@ struct Entry<int (*)(const swa_params*, A...)> {
     {
         if (!fn || n != (Py_ssize_t)N + 1) Py_RETURN_NONE;
         std::tuple<A...> a;
-        swa_params p;
+        P p;
         bool ready = false;
         try {
             ready = convert_all(args, p, a, std::make_index_sequence<N>());
@@ -133,7 +154,10 @@ struct Entry<int (*)(const swa_params*, A...)> {
     X(swa_prefill_scores) \
     X(swa_prefill_rows) \
     X(swa_prefill_attention) \
-    X(swa_quantize_kv)
+    X(swa_quantize_kv) \
+    X(swa_paged_plan) \
+    X(swa_paged_append) \
+    X(swa_paged_decode)
 
 #define SWA_DEFINE(name) \
     void* addr_##name = nullptr; \
@@ -143,13 +167,17 @@ struct Entry<int (*)(const swa_params*, A...)> {
     }
 SWA_ENTRIES(SWA_DEFINE)
 
-// bind({name: address}, SwaParams): the entry points of the library that is in use.
+// bind({name: address}, SwaParams, SwaPagedParams): the entry points of the library that is in use.
 PyObject* bind(PyObject*, PyObject* args)
 {
-    PyObject *dict = nullptr, *type = nullptr;
-    if (!PyArg_ParseTuple(args, "O!O", &PyDict_Type, &dict, &type)) return nullptr;
+    PyObject *dict = nullptr, *type = nullptr, *paged = nullptr;
+    if (!PyArg_ParseTuple(args, "O!O|O", &PyDict_Type, &dict, &type, &paged)) return nullptr;
     Py_INCREF(type);
-    Py_XSETREF(params_type, type);
+    Py_XSETREF(params_type<swa_params>, type);
+    if (paged) {
+        Py_INCREF(paged);
+        Py_XSETREF(params_type<swa_paged_params>, paged);
+    }
 #define SWA_BIND(name) \
     { \
         PyObject* v = PyDict_GetItemString(dict, #name); \
