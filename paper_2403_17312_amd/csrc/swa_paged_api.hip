@@ -115,7 +115,7 @@ int swa_paged_append(const swa_paged_params* params, swa_rows q, swa_rows k, swa
     if (n_rows < 1 || n_rows > swa::kMaxPlanRows) return SWA_ERR_BAD_SHAPE;
     // q_out may be q itself, where a row's place is the same in both
     if (q.data == q_out && q.stride != (int64_t)params->h_q * params->d) return SWA_ERR_BAD_SHAPE;
-    if (!swa::on16(q_out) || !swa::on16(q_weight) || !swa::on16(k_weight)) return SWA_ERR_ALIGNMENT;
+    if (!swa::on16(q_out) || !swa::on16(q_weight) || !swa::on16(k_weight) || !swa::on16(workspace)) return SWA_ERR_ALIGNMENT;
     return swa::launch_paged_append(*params, q, k, v, n_rows, pos, slot, inv_freq, q_weight, k_weight, q_out, k_pages, v_pages, k_scale,
                                     v_scale, workspace, static_cast<hipStream_t>(stream));
 }
@@ -130,7 +130,7 @@ int swa_paged_decode(const swa_paged_params* params, swa_rows q, int32_t n_rows,
     if ((rc = swa::check_pool(*params, k_pages, v_pages, k_scale, v_scale)) != SWA_OK) return rc;
     if ((rc = swa::check_rows(*params, q, params->h_q)) != SWA_OK) return rc;
     if (n_rows < 1 || n_rows > swa::kMaxPlanRows || (!row_start && n_rows < params->b)) return SWA_ERR_BAD_SHAPE;
-    if (!swa::on16(out)) return SWA_ERR_ALIGNMENT;
+    if (!swa::on16(out) || !swa::on16(workspace)) return SWA_ERR_ALIGNMENT;
     return swa::launch_paged_decode(*params, q, n_rows, row_start, k_pages, v_pages, k_scale, v_scale, block_table, cache_len, out, lse,
                                     workspace, static_cast<hipStream_t>(stream));
 }

@@ -146,9 +146,9 @@ def test_sizes_and_places_are_refused(B):
             assert append(B, p, rows=rows) == code, (i, row.stride)
             if i == 0:
                 assert decode(B, p, q=row) == code
-    for n in ("q_out", "k_pages", "v_pages", "q_weight", "k_weight"):
+    for n in ("q_out", "k_pages", "v_pages", "q_weight", "k_weight", "workspace"):
         assert append(B, p, **{n: ok + 8}) == B.SWA_ERR_ALIGNMENT, n
-    for n in ("k_pages", "v_pages", "out"):
+    for n in ("k_pages", "v_pages", "out", "workspace"):
         assert decode(B, p, **{n: ok + 8}) == B.SWA_ERR_ALIGNMENT, n
     rows = [R(ok, 512), R(ok, 128), R(ok, 128)]
     assert append(B, p, rows=rows, q_out=ok) == B.SWA_ERR_BAD_SHAPE      # in place, but with gaps between the rows
