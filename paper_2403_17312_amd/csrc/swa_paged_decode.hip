@@ -1,14 +1,20 @@
 // Attention of one new token per sequence over a paged cache.  Bound by HBM: every key and value of the window is read once, 4 flops for
 // two elements and query head.
 //
-// A workgroup takes a chunk of one sequence's tokens and one key/value head, with up to 16 of the query heads that share it; its
-// waves take tiles of the chunk in turn, each with a running maximum and sum of the softmax.  All products go to the matrix cores, whose
-// 16 columns are the query heads: also a single head's, since the matrix cores have fifteen times the time that HBM leaves them.
+// A workgroup serves up to 16 of the query heads that share a key head, over a range of one sequence's tokens; its four waves take tiles of the range
+// in turn, each with a running maximum and sum of the softmax.  Ranges come in two ways:
+//   chunks   few sequences: each one's tokens in equal chunks, as many as the bound on the lengths gives, a workgroup for each.
+//   shares   many, and long ones: the call's work, in steps of 128 tokens of one sequence and key head, laid end to end and cut into as
+//            many equal shares as there are workgroups, whatever the lengths are; each workgroup sums the lengths up by itself.  A share
+//            holds whole sequences and at most two pieces.  128 sequences of 512 to 8192 tokens, 8 key heads of 128 bf16 channels: chunks 425 us, shares 353 (6.5 TB/s).
+// Pieces leave partial results, which a second, small launch joins in their order.
+// All products go to the matrix cores, whose 16 columns are the query heads: also a single head's, since the matrix cores have
+// fifteen times the time that HBM leaves them.
 //   logits   S^T = K Q^T: a lane's operand is 16 bytes of one key, as it lies in memory; a 64-byte piece of 16 keys a load.
 //   values   O^T = V^T P^T: S^T leaves lane (j, c) with keys 4j..4j+3 of column c, which is what the product with V takes from that lane
 //            if its contraction runs over the keys in that order; nothing moves between lanes.  For V^T a lane loads the same D / 16
 //            channels of those keys (whole rows a load) and swaps halves of words, a byte permutation for two elements.
-// Tiles go from memory to registers and need no LDS.  Partial results of a sequence's chunks are joined by a second, small launch.
+// Tiles go from memory to registers and need no LDS.
 #include <math.h>
 
 #include <type_traits>
@@ -25,35 +31,75 @@ struct PagedArgs {
     const float *k_scale, *v_scale;
     char* out;
     float* lse;
-    float *part_out, *part_sum;                    // [b, h_q, splits, D] and [b, h_q, splits, 2] (maximum, sum) of chunks
+    float *part_out, *part_sum;                    // [pieces, row_tiles, heads, D] and [.., 2] (maximum, sum); a share's first and last piece,
+                                                   // or chunk `split` of sequence and key head
+    int4* begun;                                   // [shares]: key head, row, pieces of the sequence that a share begins and does not end (x = 0: none)
     int32_t* status;
     int32_t b, n_rows, h_q, h_kv, page_size, n_pages, max_pages, window, len_max;
-    int32_t group, row_tiles, splits, chunk;       // query heads of a key head, tiles of 16 of them, chunks at most, tokens of one
+    int32_t group, row_tiles, heads;               // query heads of a key head, tiles of 16 of them, heads of a tile at most
+    int32_t ranges;                                // shares, or chunks of a sequence at most
+    int32_t chunk;                                 // tokens
     uint32_t page_mul;                             // t / page_size = t * page_mul >> page_shift for 0 <= t < 2^31
     int32_t page_shift;
+    int32_t sixteens;                              // pages are whole sixteens of tokens
     float scale;                                   // of logits to the base 2
 };
 
 constexpr int kPagedWaves = 4;
-constexpr int kPagedTargetGroups = 1024;           // workgroups that fill the chip: four on every CU
-constexpr int kPagedMaxSplits = 256;
+constexpr int kPagedStep = 128;                    // tokens
+constexpr int kPagedChunks = 256;                  // chunks of a sequence at most, which bounds what the join of one has to read
 
-static int64_t paged_units(const swa_paged_params& p)
+static int row_tiles_of(const swa_paged_params& p) { return (p.h_q / p.h_kv + 15) / 16; }
+
+// Tokens of a sequence that a call may see, from a multiple of 32 on.
+static int64_t paged_span(const swa_paged_params& p)
 {
-    const int group = p.h_q / p.h_kv;
-    return (int64_t)p.b * p.h_kv * ((group + 15) / 16);
+    int64_t n = (int64_t)p.max_pages * p.page_size;
+    if (p.len_bound > 0 && p.len_bound < n) n = p.len_bound;
+    return p.window > 0 && p.window < n ? (int64_t)p.window + 31 : n;
 }
 
-static int paged_max_splits(const swa_paged_params& p)
+// Shares take a launch's time longer to begin (the sums) and to end (pieces), and level the lengths out.  us, chunks / shares, 32 query and 8 key
+// heads of 128 bf16 channels, lengths even over 100..8001, and all 4000: 4 sequences 25.9 / 27.4, 19.7 / 19.9; 8: 33.3 / 32.0, 28.6 / 31.4; 16: 58.8 / 53.7, 47.9 /
+// 50.5; 32: 113 / 95, 87 / 90; 64: 217 / 178, 174 / 176; 128: 398 / 345, 331 / 338.  16 sequences of 32 fp32 heads, 64 channels, a window of 512: 27.2 / 30.5.
+static bool paged_in_shares(const swa_paged_params& p)
 {
-    const int64_t s = (kPagedTargetGroups + paged_units(p) - 1) / paged_units(p);
-    return s < kPagedMaxSplits ? (int)s : kPagedMaxSplits;
+    return (int64_t)p.b * p.h_kv * row_tiles_of(p) >= 64 && paged_span(p) >= 1024;
+}
+
+static int64_t paged_units(const swa_paged_params& p) { return (int64_t)p.b * p.h_kv * row_tiles_of(p); }
+
+constexpr bool paged_two(int row_bytes) { return row_bytes == 512; }
+
+// Shares of a call at most: the workgroups that the chip holds at once.  A CU has four of 64 channels, three of 128 (168 registers a lane), two of 128
+// in fp32, which do not fit those (64 sequences of 4352 tokens, 8 key heads: three with spills 381 us, two 356).  768 / 1024 shares of 128
+// channels: the ragged 128 sequences below 345 / 387 us; 64 of 100..8001 tokens in 8 bits 107 / 123.
+static int paged_max_shares(const swa_paged_params& p)
+{
+    const int n = (p.d == 64 ? 1024 : paged_two(paged_row_bytes(p)) ? 512 : 768) / row_tiles_of(p);
+    return n < 1 ? 1 : n;
+}
+
+// Chunks of a sequence at most.
+static int paged_max_chunks(const swa_paged_params& p)
+{
+    const int64_t n = (1024 + paged_units(p) - 1) / paged_units(p);
+    return n > kPagedChunks ? kPagedChunks : (int)n;
+}
+
+// (for either form, whatever length and window a call states)
+static int64_t paged_piece_rows(const swa_paged_params& p)
+{
+    const int group = p.h_q / p.h_kv;
+    const int64_t shares = 2 * (int64_t)paged_max_shares(p) * row_tiles_of(p);
+    const int64_t chunks = paged_max_chunks(p) > 1 ? paged_max_chunks(p) * paged_units(p) : 0;
+    const int64_t pieces = paged_units(p) >= 64 && shares > chunks ? shares : chunks;
+    return 2 * ((pieces * (group < 16 ? group : 16) + 1) / 2);
 }
 
 size_t paged_partial_bytes(const swa_paged_params& p)
 {
-    const int s = paged_max_splits(p);
-    return s == 1 ? 0 : (size_t)p.b * p.h_q * s * (p.d + 2) * sizeof(float);
+    return (size_t)paged_piece_rows(p) * (p.d + 2) * sizeof(float) + (size_t)paged_max_shares(p) * sizeof(int4);
 }
 
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
@@ -80,277 +126,407 @@ __device__ __forceinline__ uint32_t round2(float lo, float hi)
     else return f32x2_to_bf16x2_bits(lo, hi);
 }
 
+template <typename V>
+__device__ __forceinline__ V load_values(const char* p)
+{
+    typedef uint32_t words_t __attribute__((ext_vector_type(sizeof(V) / 4)));
+    if constexpr (sizeof(V) == 4) return V{{__builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p))}};
+    else return __builtin_bit_cast(V, __builtin_nontemporal_load(reinterpret_cast<const words_t*>(p)));
+}
+
 __device__ __forceinline__ float code(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
 
-// What a sequence asks of this call: its row, and its tokens lo .. n-1.  False: nothing.
-__device__ __forceinline__ bool paged_sequence(const PagedArgs& a, int s, int& row, int& lo, int& n, bool& too_long)
+// What a sequence asks of this call: its row, its tokens lo .. n-1, and steps (0: nothing).
+__device__ __forceinline__ int paged_sequence(const PagedArgs& a, int s, int& row, int& lo, int& n, bool& too_long)
 {
     n = a.cache_len[s];
     row = s;
-    too_long = false;
     if (a.row_start) {
         row = a.row_start[s + 1] - 1;
-        if (row < a.row_start[s]) return false;
+        if (row < a.row_start[s]) return 0;
     }
-    if (n < 0 || row < 0 || row >= a.n_rows) return false;
+    if (n < 0 || row < 0 || row >= a.n_rows) return 0;
     if (n > a.len_max) {
         too_long = true;
-        return false;
+        return 0;
     }
     lo = a.window && n > a.window ? n - a.window : 0;
-    return true;
+    const int tokens = n - (lo & ~31);                   // (tiles begin at multiples of 32)
+    return tokens > kPagedStep ? (tokens + kPagedStep - 1) / kPagedStep : 1;
 }
 
-// T: type of queries and outputs, C: of the pages (Q8: codes), M: of the operands in the matrix cores.
-template <typename T, typename C, int D>
-__global__ void __launch_bounds__(64 * kPagedWaves) swa_paged_decode_kernel(PagedArgs a)
+// The shares: the first `more` of them have one step more than the others.
+struct Shares {
+    int steps, more;
+    __device__ __forceinline__ int begin(int g) const { return g * steps + (g < more ? g : more); }
+    __device__ __forceinline__ int of(int x) const
+    {
+        const int longer = more * (steps + 1);
+        return x < longer ? x / (steps + 1) : more + (x - longer) / steps;
+    }
+};
+
+// T: type of queries and outputs, C: of the pages (Q8: codes).
+template <typename T, typename C, int D, bool SHARES>
+__global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * D) ? 2 : 3) swa_paged_decode_kernel(PagedArgs a)
 {
     constexpr bool kCodes = std::is_same_v<C, Q8>, kWide = std::is_same_v<C, F32>;
-    // Codes are exact in bf16.  fp16 queries have three bits more than that and the weights are products with a scale: both go as two bf16
-    // numbers, which hold 16 bits.
-    typedef std::conditional_t<kCodes, BF16, T> M;
-    constexpr bool kSplitQ = kCodes && std::is_same_v<T, F16>;
+    // Codes are exact in either 16-bit type.  Keys get the queries' type; values get bf16, whose range the weights need, which are products with a
+    // scale there, and the weights go as two bf16 numbers, which hold 16 bits.
     constexpr int kKeys = kWide ? 16 : 32, kTiles = kKeys / 16, kRow = D * Elem<C>::kBytes;
     constexpr int kSteps = kWide ? D / 16 : D / 32;      // operands of a logit
     constexpr int kChannels = D / 16;                    // of V in a lane
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, j = lane >> 4;
 
-    // Row tiles of one chunk read the same pages: eight chunks, then the same ones' next row tile, so that they meet in one XCD's L2.
-    const int eighth = blockIdx.x >> 3, units = a.b * a.h_kv;
-    const int work = (eighth / a.row_tiles) * 8 + (blockIdx.x & 7), tile = eighth % a.row_tiles;
-    const int split = work / units, unit = work - split * units;
-    if (split >= a.splits) return;
-    const int s = unit / a.h_kv, kv = unit - s * a.h_kv;
-    int row, lo, n;
-    bool too_long;
-    if (!paged_sequence(a, s, row, lo, n, too_long)) {
-        if (too_long && split == 0 && tid == 0) atomicOr(a.status, kStatusCapacityBit);
-        return;
-    }
-    const int base0 = lo & ~31, chunks = n > base0 ? (n - base0 + a.chunk - 1) / a.chunk : 1;
-    if (split >= chunks) return;
-    const int begin = base0 + split * a.chunk, end = n - begin < a.chunk ? n : begin + a.chunk;
-
-    // Query operands: column col is query head 16 tile + col of the group.
+    // Row tiles of one range read the same pages: eight ranges, then the same ones' next row tile, so that they meet in one XCD's L2.
+    const int eighth = blockIdx.x >> 3, work = (eighth / a.row_tiles) * 8 + (blockIdx.x & 7), tile = eighth % a.row_tiles;
     const int heads = a.group - 16 * tile < 16 ? a.group - 16 * tile : 16;
-    const int64_t head0 = (int64_t)kv * a.group + 16 * tile;
-    Vec16 q[kSteps], q_rest[kSplitQ ? kSteps : 1];
-    {
-        const char* const from = a.q + row * a.q_stride + (head0 + col) * (D * Elem<T>::kBytes);
-#pragma unroll
-        for (int c = 0; c < kSteps; ++c) {
-            // (16 bytes of codes are two operands' channels)
-            const int at = kCodes ? (c / 2) * 64 + j * 16 + (c & 1) * 8 : kWide ? c * 16 + j * 4 : c * 32 + j * 8;
-            q[c] = col < heads ? load16(from + at * Elem<T>::kBytes) : Vec16{0u, 0u, 0u, 0u};
-            if constexpr (kSplitQ) {
-                float f[8], rest[8];
-                unpack<F16>(q[c], f);
-                q[c] = pack<BF16>(f);
-                unpack<BF16>(q[c], rest);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) rest[i] = f[i] - rest[i];
-                q_rest[c] = pack<BF16>(rest);
-            }
-        }
-    }
 
-    float top = -INFINITY, sum = 0.f;                    // of column col, the sum of this lane's keys alone
-    f32x4_t acc[kChannels];
-#pragma unroll
-    for (int e = 0; e < kChannels; ++e) acc[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-    const int32_t* const table = a.block_table + (int64_t)s * a.max_pages;
-    bool bad = false;
-
-    // Row of the pool that holds this lane's token of the tile at `base` (-1: none).
-    auto token_page = [&](int base, int& off) {
-        const int t = base + (lane & (kKeys - 1));
-        const int clamped = t < lo ? lo : (t < n ? t : n - 1);
-        const int page = (int)(((uint64_t)(uint32_t)clamped * a.page_mul) >> a.page_shift);
-        off = clamped - page * a.page_size;
-        return table[page];
-    };
-    int next_off = 0, next_page = begin + wave * kKeys < end ? token_page(begin + wave * kKeys, next_off) : 0;
-    for (int base = begin + wave * kKeys; base < end; base += kPagedWaves * kKeys) {
-        const int page = next_page, off = next_off;
-        if (base + kPagedWaves * kKeys < end) next_page = token_page(base + kPagedWaves * kKeys, next_off);
-        const int t = base + (lane & (kKeys - 1));
-        const bool in_pool = (uint32_t)page < (uint32_t)a.n_pages, live = t >= lo && t < n;
-        bad |= live && !in_pool;
-        const int r = in_pool && live ? (page * a.h_kv + kv) * a.page_size + off : -1;
-        const bool edge = __any(r < 0);
-
-        int rk[kTiles], rv[kTiles][4];
-#pragma unroll
-        for (int u = 0; u < kTiles; ++u) {
-            rk[u] = __shfl(r, u * 16 + col, 64);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) rv[u][i] = __shfl(r, u * 16 + j * 4 + i, 64);
-        }
-        // keys, then values: all of a tile's loads before its first product
-        constexpr int kLoads = kCodes ? D / 64 : kSteps, kVLoad = kWide ? D / 64 : 1, kVBytes = kWide ? 16 : kChannels * Elem<C>::kBytes;
-        Vec16 k[kTiles][kLoads];
-        struct alignas(kVBytes < 16 ? kVBytes : 16) Values { uint32_t w[kVBytes / 4]; } v[kTiles][4][kVLoad];
-#pragma unroll
-        for (int u = 0; u < kTiles; ++u) {
-            const char* const from = a.k_pages + (int64_t)(rk[u] < 0 ? 0 : rk[u]) * kRow + j * 16;
-#pragma unroll
-            for (int c = 0; c < kLoads; ++c) k[u][c] = load16_stream(from + c * 64);
-        }
-#pragma unroll
-        for (int u = 0; u < kTiles; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const char* const from = a.v_pages + (int64_t)(rv[u][i] < 0 ? 0 : rv[u][i]) * kRow + col * kVBytes;
-#pragma unroll
-                for (int x = 0; x < kVLoad; ++x) v[u][i][x] = *reinterpret_cast<const Values*>(from + x * 256);
-            }
-        float k_scale = 0.f, v_scale = 0.f;
-        if constexpr (kCodes) {
-            k_scale = r < 0 ? 0.f : a.k_scale[r];
-            v_scale = r < 0 ? 0.f : a.v_scale[r];
-        }
-
-        float x[kTiles][4];
-#pragma unroll
-        for (int u = 0; u < kTiles; ++u) {
-            f32x4_t logit = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int c = 0; c < kSteps; ++c) {
-                if constexpr (kCodes) {
-                    const Vec16& b = k[u][c / 2];
-                    const uint32_t w[2] = {c & 1 ? b.z : b.x, c & 1 ? b.w : b.y};
-                    const Vec16 op = {round2<BF16>(code(w[0], 0), code(w[0], 1)), round2<BF16>(code(w[0], 2), code(w[0], 3)),
-                                      round2<BF16>(code(w[1], 0), code(w[1], 1)), round2<BF16>(code(w[1], 2), code(w[1], 3))};
-                    logit = mfma16<BF16>(op, q[c], logit);
-                    if constexpr (kSplitQ) logit = mfma16<BF16>(op, q_rest[c], logit);
-                } else {
-                    logit = mfma16<M>(k[u][c], q[c], logit);
-                }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[u][i] = logit[i] * (kCodes ? a.scale * __shfl(k_scale, u * 16 + j * 4 + i, 64) : a.scale);
-                if (edge && rv[u][i] < 0) x[u][i] = -INFINITY;
-            }
-        }
-        float most = x[0][0];
-#pragma unroll
-        for (int i = 1; i < 4 * kTiles; ++i) most = fmaxf(most, x[i / 4][i % 4]);
-        most = fmaxf(most, __shfl_xor(most, 16, 64));
-        most = fmaxf(most, __shfl_xor(most, 32, 64));
-        if (__any(most > top)) {
-            const float to = fmaxf(top, most), down = __builtin_amdgcn_exp2f(top - (to == -INFINITY ? 0.f : to));
-            top = to;
-            sum *= down;
-#pragma unroll
-            for (int e = 0; e < kChannels; ++e) acc[e] *= down;
-        }
-        const float from = top == -INFINITY ? 0.f : top;
-#pragma unroll
-        for (int u = 0; u < kTiles; ++u)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[u][i] = __builtin_amdgcn_exp2f(x[u][i] - from);
-                sum += x[u][i];
-                if constexpr (kCodes) x[u][i] *= __shfl(v_scale, u * 16 + j * 4 + i, 64);
-                if (edge && rv[u][i] < 0) {
-                    x[u][i] = 0.f;
-#pragma unroll
-                    for (int y = 0; y < kVLoad; ++y) v[u][i][y] = Values{};
-                }
-            }
-
-        if constexpr (kWide) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int e = 0; e < kChannels; ++e)
-                    acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(u2f(v[0][i][e / 4].w[e % 4]), x[0][i], acc[e], 0, 0, 0);
-        } else if constexpr (kCodes) {
-            Vec16 p = {round2<BF16>(x[0][0], x[0][1]), round2<BF16>(x[0][2], x[0][3]), round2<BF16>(x[1][0], x[1][1]), round2<BF16>(x[1][2], x[1][3])};
-            float f[8];
-            unpack<BF16>(p, f);
-            const Vec16 p_rest = {round2<BF16>(x[0][0] - f[0], x[0][1] - f[1]), round2<BF16>(x[0][2] - f[2], x[0][3] - f[3]),
-                                  round2<BF16>(x[1][0] - f[4], x[1][1] - f[5]), round2<BF16>(x[1][2] - f[6], x[1][3] - f[7])};
-#pragma unroll
-            for (int e = 0; e < kChannels; ++e) {
-                auto c = [&](int u, int i) { return code(v[u][i][0].w[e / 4], e % 4); };
-                const Vec16 op = {round2<BF16>(c(0, 0), c(0, 1)), round2<BF16>(c(0, 2), c(0, 3)), round2<BF16>(c(1, 0), c(1, 1)),
-                                  round2<BF16>(c(1, 2), c(1, 3))};
-                acc[e] = mfma16<BF16>(op, p, acc[e]);
-                acc[e] = mfma16<BF16>(op, p_rest, acc[e]);
-            }
-        } else {
-            const Vec16 p = {round2<M>(x[0][0], x[0][1]), round2<M>(x[0][2], x[0][3]), round2<M>(x[1][0], x[1][1]), round2<M>(x[1][2], x[1][3])};
-#pragma unroll
-            for (int e = 0; e < kChannels; ++e) {
-                constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;
-                auto two = [&](int u, int i) { return __builtin_amdgcn_perm(v[u][i + 1][0].w[e / 2], v[u][i][0].w[e / 2], e & 1 ? kHigh : kLow); };
-                acc[e] = mfma16<M>(Vec16{two(0, 0), two(0, 2), two(1, 0), two(1, 2)}, p, acc[e]);
-            }
-        }
-    }
-    if (bad) atomicOr(a.status, kStatusBadRequestBit);
-
-    // The waves' results to one, in LDS: rows are query heads.
     constexpr int kPitch = D + 4;
     __shared__ float part[kPagedWaves][16][kPitch];
     __shared__ float tops[kPagedWaves][16], sums[kPagedWaves][16];
-    sum += __shfl_xor(sum, 16, 64);
-    sum += __shfl_xor(sum, 32, 64);
-    if (j == 0) {
-        tops[wave][col] = top;
-        sums[wave][col] = sum;
+    extern __shared__ int before[];                      // shares: steps of a key head before sequence s, for s <= b
+
+    int s = 0, kv = 0, row, lo, n, split = 0, x = 0, x1 = 0;
+    bool too_long = false;
+    Shares shares{0, 0};
+    int4 begun = {0, 0, 0, 0};
+    if constexpr (SHARES) {
+        if (work >= a.ranges) return;
+        __shared__ int wave_steps[kPagedWaves];
+        const int per = (a.b + 64 * kPagedWaves - 1) / (64 * kPagedWaves), s0 = tid * per, s1 = s0 + per < a.b ? s0 + per : a.b;
+        int own = 0;
+        for (int i = s0; i < s1; ++i) {
+            own += paged_sequence(a, i, row, lo, n, too_long);
+            before[i + 1] = own;
+        }
+        if (too_long && blockIdx.x == 0) atomicOr(a.status, kStatusCapacityBit);
+        int to = own;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int up = __shfl_up(to, o, 64);
+            if (lane >= o) to += up;
+        }
+        if (lane == 63) wave_steps[wave] = to;
+        __syncthreads();
+        int add = to - own;
+        for (int w = 0; w < wave; ++w) add += wave_steps[w];
+        for (int i = s0; i < s1; ++i) before[i + 1] += add;
+        if (tid == 0) before[0] = 0;
+        __syncthreads();
+        const int total = __builtin_amdgcn_readfirstlane(before[a.b]) * a.h_kv;
+        shares = Shares{total / a.ranges, total % a.ranges};
+        x = shares.begin(work);
+        x1 = shares.begin(work + 1);
+        for (int above = a.b; s + 1 < above;) {          // the sequence that x lies in
+            const int mid = (s + above) >> 1;
+            if (before[mid] * a.h_kv <= x) s = mid; else above = mid;
+        }
+        s = __builtin_amdgcn_readfirstlane(s);
+    } else {
+        const int units = a.b * a.h_kv;
+        split = work / units;
+        if (split >= a.ranges) return;
+        s = (work - split * units) / a.h_kv;
+        kv = work - split * units - s * a.h_kv;
     }
+
+    do {
+        int begin, end;
+        bool whole;                                          // all of the sequence
+        int64_t piece = 0;
+        if constexpr (SHARES) {
+            if (x >= x1) break;
+            const int s_before = __builtin_amdgcn_readfirstlane(before[s]), steps = __builtin_amdgcn_readfirstlane(before[s + 1]) - s_before;
+            if (steps == 0) {
+                ++s;
+                continue;
+            }
+            const int in_s = x - s_before * a.h_kv;
+            kv = in_s / steps;
+            const int first = in_s - kv * steps, last = steps - first < x1 - x ? steps : first + (x1 - x);
+            whole = first == 0 && last == steps;
+            piece = 2 * work + (first == 0);
+            paged_sequence(a, s, row, lo, n, too_long);
+            begin = (lo & ~31) + first * kPagedStep;
+            end = last == steps ? n : (lo & ~31) + last * kPagedStep;
+            if (first == 0 && last < steps) begun = int4{1 + kv, row, shares.of(x + steps - 1) - work + 1, 0};
+            x += last - first;
+        } else {
+            if (!paged_sequence(a, s, row, lo, n, too_long)) {
+                if (too_long && split == 0 && tid == 0) atomicOr(a.status, kStatusCapacityBit);
+                return;
+            }
+            const int from = lo & ~31;
+            begin = from + split * a.chunk;
+            if (split > 0 && begin >= n) return;
+            end = n - begin < a.chunk ? n : begin + a.chunk;
+            whole = n - from <= a.chunk;
+            piece = ((int64_t)s * a.h_kv + kv) * a.ranges + split;
+        }
+
+        // Query operands: column col is query head 16 tile + col of the group.
+        const int64_t head0 = (int64_t)kv * a.group + 16 * tile;
+        Vec16 q[kSteps];
+        {
+            const char* const from = a.q + row * a.q_stride + (head0 + col) * (D * Elem<T>::kBytes);
 #pragma unroll
-    for (int e = 0; e < kChannels; ++e)
+            for (int c = 0; c < kSteps; ++c) {
+                // (16 bytes of codes are two operands' channels)
+                const int at = kCodes ? (c / 2) * 64 + j * 16 + (c & 1) * 8 : kWide ? c * 16 + j * 4 : c * 32 + j * 8;
+                q[c] = col < heads ? load16(from + at * Elem<T>::kBytes) : Vec16{0u, 0u, 0u, 0u};
+            }
+        }
+
+        float top = -INFINITY, sum = 0.f;                    // of column col, the sum of this lane's keys alone
+        f32x4_t acc[kChannels];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) part[wave][col][kWide ? (e / 4) * 64 + (4 * j + i) * 4 + e % 4 : (4 * j + i) * kChannels + e] = acc[e][i];
-    __syncthreads();
-    const int head = tid >> 4;
-    if (head >= heads) return;
-    float all = tops[0][head];
+        for (int e = 0; e < kChannels; ++e) acc[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        const int32_t* const table = a.block_table + (int64_t)s * a.max_pages;
+        bool bad = false;
+
+        // Row of the pool that holds this lane's token of the tile at `base` (-1: none).
+        auto token_page = [&](int base, int& off) {
+            const int t = base + (lane & (kKeys - 1));
+            const int clamped = t < lo ? lo : (t < n ? t : n - 1);
+            const int page = (int)(((uint64_t)(uint32_t)clamped * a.page_mul) >> a.page_shift);
+            off = clamped - page * a.page_size;
+            return table[page];
+        };
+        constexpr int kLoads = kCodes ? D / 64 : kSteps, kVLoad = kWide ? D / 64 : 1, kVBytes = kWide ? 16 : kChannels * Elem<C>::kBytes;
+        struct alignas(kVBytes < 16 ? kVBytes : 16) Values { uint32_t w[kVBytes / 4]; };
+
+        // One tile, whose tokens lie in rows r (of lane t % kKeys) of the pool.  In `whole` tiles all of them do, and sixteen at a time behind each
+        // other, so that addresses are a scalar and a lane's constant; in others each lane fetches its rows' numbers, and rows of -1 are left out.
+        auto take = [&](auto whole, const int r) __attribute__((always_inline)) {
+            constexpr bool kWhole = decltype(whole)::value;
+            int rv[kTiles][4];
+            Vec16 k[kTiles][kLoads];
+            Values v[kTiles][4][kVLoad];
+            f32x4_t k_scale[kTiles], v_scale[kTiles];
 #pragma unroll
-    for (int w = 1; w < kPagedWaves; ++w) all = fmaxf(all, tops[w][head]);
-    float total = 0.f, y[kChannels] = {};
+            for (int u = 0; u < kTiles; ++u) {
+                const char* k_from;
+                if constexpr (kWhole) {
+                    const int64_t first = __builtin_amdgcn_readlane(r, u * 16);
+                    k_from = a.k_pages + first * kRow + (uint32_t)(col * kRow + j * 16);
+                } else {
+                    const int rk = __shfl(r, u * 16 + col, 64);
+                    k_from = a.k_pages + (int64_t)(rk < 0 ? 0 : rk) * kRow + j * 16;
+                }
 #pragma unroll
-    for (int w = 0; w < kPagedWaves; ++w) {
-        const float f = __builtin_amdgcn_exp2f(tops[w][head] - (all == -INFINITY ? 0.f : all));
-        total = __builtin_fmaf(sums[w][head], f, total);
+                for (int c = 0; c < kLoads; ++c) k[u][c] = load16_stream(k_from + c * 64);
+            }
 #pragma unroll
-        for (int e = 0; e < kChannels; ++e) y[e] = __builtin_fmaf(part[w][head][(tid & 15) * kChannels + e], f, y[e]);
-    }
-    const int64_t hq = head0 + head;
-    if (chunks == 1) {
-        const float inverse = total == 0.f ? 0.f : 1.f / total;
-        char* const to = a.out + ((int64_t)row * a.h_q + hq) * (D * Elem<T>::kBytes);
+            for (int u = 0; u < kTiles; ++u) {
+                const int64_t first = kWhole ? __builtin_amdgcn_readlane(r, u * 16) : 0;
 #pragma unroll
-        for (int e = 0; e < kChannels; ++e) store_elem<T>(to, (tid & 15) * kChannels + e, total == 0.f ? 0.f : y[e] * inverse);
-        if (a.lse && (tid & 15) == 0) a.lse[(int64_t)row * a.h_q + hq] = (all + __builtin_log2f(total)) * 0.69314718055994530942f;
-        return;
-    }
-    const int64_t at = ((int64_t)s * a.h_q + hq) * a.splits + split;
+                for (int i = 0; i < 4; ++i) {
+                    const char* v_from;
+                    if constexpr (kWhole) {
+                        v_from = a.v_pages + first * kRow + (uint32_t)(j * 4 * kRow + col * kVBytes) + i * kRow;
+                    } else {
+                        rv[u][i] = __shfl(r, u * 16 + j * 4 + i, 64);
+                        v_from = a.v_pages + (int64_t)(rv[u][i] < 0 ? 0 : rv[u][i]) * kRow + col * kVBytes;
+                    }
 #pragma unroll
-    for (int e = 0; e < kChannels; e += 4)
-        *reinterpret_cast<f32x4_t*>(a.part_out + at * D + (tid & 15) * kChannels + e) = f32x4_t{y[e], y[e + 1], y[e + 2], y[e + 3]};
-    if ((tid & 15) == 0) *reinterpret_cast<float2*>(a.part_sum + at * 2) = float2{all, total};
+                    for (int x = 0; x < kVLoad; ++x) v[u][i][x] = load_values<Values>(v_from + x * 256);
+                }
+                if constexpr (kCodes) {
+                    if constexpr (kWhole) {
+                        k_scale[u] = *reinterpret_cast<const f32x4_t*>(a.k_scale + first + 4 * j);
+                        v_scale[u] = *reinterpret_cast<const f32x4_t*>(a.v_scale + first + 4 * j);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            k_scale[u][i] = rv[u][i] < 0 ? 0.f : a.k_scale[rv[u][i]];
+                            v_scale[u][i] = rv[u][i] < 0 ? 0.f : a.v_scale[rv[u][i]];
+                        }
+                    }
+                }
+            }
+
+            __builtin_amdgcn_sched_barrier(0);
+            float x[kTiles][4];
+#pragma unroll
+            for (int u = 0; u < kTiles; ++u) {
+                f32x4_t logit = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < kSteps; ++c) {
+                    if constexpr (kCodes) {
+                        const Vec16& b = k[u][c / 2];
+                        const uint32_t w[2] = {c & 1 ? b.z : b.x, c & 1 ? b.w : b.y};
+                        const Vec16 op = {round2<T>(code(w[0], 0), code(w[0], 1)), round2<T>(code(w[0], 2), code(w[0], 3)),
+                                          round2<T>(code(w[1], 0), code(w[1], 1)), round2<T>(code(w[1], 2), code(w[1], 3))};
+                        logit = mfma16<T>(op, q[c], logit);
+                    } else {
+                        logit = mfma16<T>(k[u][c], q[c], logit);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[u][i] = logit[i] * a.scale;
+                    if constexpr (kCodes) x[u][i] *= k_scale[u][i];
+                    if constexpr (!kWhole) x[u][i] = rv[u][i] < 0 ? -INFINITY : x[u][i];
+                }
+            }
+            float most = x[0][0];
+#pragma unroll
+            for (int i = 1; i < 4 * kTiles; ++i) most = fmaxf(most, x[i / 4][i % 4]);
+            most = fmaxf(most, __shfl_xor(most, 16, 64));
+            most = fmaxf(most, __shfl_xor(most, 32, 64));
+            if (__any(most > top)) {
+                const float to = fmaxf(top, most), down = __builtin_amdgcn_exp2f(top - (to == -INFINITY ? 0.f : to));
+                top = to;
+                sum *= down;
+#pragma unroll
+                for (int e = 0; e < kChannels; ++e) acc[e] *= down;
+            }
+            const float from = top == -INFINITY ? 0.f : top;
+#pragma unroll
+            for (int u = 0; u < kTiles; ++u)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[u][i] = __builtin_amdgcn_exp2f(x[u][i] - from);
+                    sum += x[u][i];
+                    if constexpr (kCodes) x[u][i] *= v_scale[u][i];
+                    if constexpr (!kWhole) {                 // (a weight of 0 times what is no number is none either)
+                        const uint32_t keep = rv[u][i] < 0 ? 0u : ~0u;
+#pragma unroll
+                        for (int y = 0; y < kVLoad; ++y)
+#pragma unroll
+                            for (int z = 0; z < kVBytes / 4; ++z) v[u][i][y].w[z] &= keep;
+                    }
+                }
+
+            if constexpr (kWide) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int e = 0; e < kChannels; ++e)
+                        acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(u2f(v[0][i][e / 4].w[e % 4]), x[0][i], acc[e], 0, 0, 0);
+            } else if constexpr (kCodes) {
+                const Vec16 p = {round2<BF16>(x[0][0], x[0][1]), round2<BF16>(x[0][2], x[0][3]), round2<BF16>(x[1][0], x[1][1]), round2<BF16>(x[1][2], x[1][3])};
+                float f[8];
+                unpack<BF16>(p, f);
+                const Vec16 p_rest = {round2<BF16>(x[0][0] - f[0], x[0][1] - f[1]), round2<BF16>(x[0][2] - f[2], x[0][3] - f[3]),
+                                      round2<BF16>(x[1][0] - f[4], x[1][1] - f[5]), round2<BF16>(x[1][2] - f[6], x[1][3] - f[7])};
+#pragma unroll
+                for (int e = 0; e < kChannels; ++e) {
+                    auto c = [&](int u, int i) { return code(v[u][i][0].w[e / 4], e % 4); };
+                    const Vec16 op = {round2<BF16>(c(0, 0), c(0, 1)), round2<BF16>(c(0, 2), c(0, 3)), round2<BF16>(c(1, 0), c(1, 1)),
+                                      round2<BF16>(c(1, 2), c(1, 3))};
+                    acc[e] = mfma16<BF16>(op, p, acc[e]);
+                    acc[e] = mfma16<BF16>(op, p_rest, acc[e]);
+                }
+            } else {
+                const Vec16 p = {round2<T>(x[0][0], x[0][1]), round2<T>(x[0][2], x[0][3]), round2<T>(x[1][0], x[1][1]), round2<T>(x[1][2], x[1][3])};
+#pragma unroll
+                for (int e = 0; e < kChannels; ++e) {
+                    constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;
+                    auto two = [&](int u, int i) { return __builtin_amdgcn_perm(v[u][i + 1][0].w[e / 2], v[u][i][0].w[e / 2], e & 1 ? kHigh : kLow); };
+                    acc[e] = mfma16<T>(Vec16{two(0, 0), two(0, 2), two(1, 0), two(1, 2)}, p, acc[e]);
+                }
+            }
+        };
+
+        // Whole tiles first; the others, at the ends of the window and where a page is not in the pool, in a loop of their own, whose addresses then
+        // take no registers from this one.
+        constexpr int kStride = kPagedWaves * kKeys;
+        const int tile0 = begin + wave * kKeys;
+        auto row_of = [&](int base, int page, int off) {
+            const int t = base + (lane & (kKeys - 1));
+            return (uint32_t)page < (uint32_t)a.n_pages && t >= lo && t < n ? (page * a.h_kv + kv) * a.page_size + off : -1;
+        };
+        int left0 = tile0, left1 = end;                      // tiles that are left
+        if (a.sixteens) {
+            left0 = end;
+            left1 = begin;
+            int next_off = 0, next_page = tile0 < end ? token_page(tile0, next_off) : 0;
+            for (int base = tile0; base < end; base += kStride) {
+                const int page = next_page, off = next_off;
+                if (base + kStride < end) next_page = token_page(base + kStride, next_off);
+                const int r = row_of(base, page, off);
+                if (!__any(r < 0)) {
+                    take(std::true_type{}, r);
+                } else {
+                    left0 = base < left0 ? base : left0;
+                    left1 = base + 1;
+                }
+            }
+        }
+        for (int base = left0; base < left1; base += kStride) {
+            int off = 0;
+            const int page = token_page(base, off), r = row_of(base, page, off), t = base + (lane & (kKeys - 1));
+            if (a.sixteens && !__any(r < 0)) continue;
+            bad |= (uint32_t)page >= (uint32_t)a.n_pages && t >= lo && t < n;
+            take(std::false_type{}, r);
+        }
+        if (bad) atomicOr(a.status, kStatusBadRequestBit);
+
+        // The waves' results to one, in LDS: rows are query heads.
+        int who = tid;
+        if (SHARES) asm volatile("" : "+v"(who));            // (addresses made from it are not kept in registers around the loop)
+        const int to_col = who & 15, to_j = (who >> 4) & 3;
+        sum += __shfl_xor(sum, 16, 64);
+        sum += __shfl_xor(sum, 32, 64);
+        __syncthreads();                                     // (the piece before this one has been read)
+        if (to_j == 0) {
+            tops[wave][to_col] = top;
+            sums[wave][to_col] = sum;
+        }
+#pragma unroll
+        for (int e = 0; e < kChannels; ++e)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) part[wave][to_col][kWide ? (e / 4) * 64 + (4 * to_j + i) * 4 + e % 4 : (4 * to_j + i) * kChannels + e] = acc[e][i];
+        __syncthreads();
+        const int head = who >> 4;
+        if (head < heads) {
+            float all = tops[0][head];
+#pragma unroll
+            for (int w = 1; w < kPagedWaves; ++w) all = fmaxf(all, tops[w][head]);
+            float total = 0.f, y[kChannels] = {};
+#pragma unroll
+            for (int w = 0; w < kPagedWaves; ++w) {
+                const float f = __builtin_amdgcn_exp2f(tops[w][head] - (all == -INFINITY ? 0.f : all));
+                total = __builtin_fmaf(sums[w][head], f, total);
+#pragma unroll
+                for (int e = 0; e < kChannels; ++e) y[e] = __builtin_fmaf(part[w][head][(who & 15) * kChannels + e], f, y[e]);
+            }
+            if (whole) {
+                const int64_t at = (int64_t)row * a.h_q + head0 + head;
+                const float inverse = 1.f / total;
+                char* const to = a.out + at * (D * Elem<T>::kBytes);
+#pragma unroll
+                for (int e = 0; e < kChannels; ++e) store_elem<T>(to, (who & 15) * kChannels + e, total == 0.f ? 0.f : y[e] * inverse);
+                if (a.lse && (who & 15) == 0) a.lse[at] = (all + __builtin_log2f(total)) * 0.69314718055994530942f;
+            } else {
+                const int64_t at = (piece * a.row_tiles + tile) * a.heads + head;
+#pragma unroll
+                for (int e = 0; e < kChannels; e += 4)
+                    *reinterpret_cast<f32x4_t*>(a.part_out + at * D + (who & 15) * kChannels + e) = f32x4_t{y[e], y[e + 1], y[e + 2], y[e + 3]};
+                if ((who & 15) == 0) *reinterpret_cast<float2*>(a.part_sum + at * 2) = float2{all, total};
+            }
+        }
+        if (SHARES && kv == a.h_kv - 1 && x == before[s + 1] * a.h_kv) ++s;
+    } while (SHARES);
+    if (SHARES && tile == 0 && tid == 0) a.begun[work] = begun;
 }
 
-// Chunks of a sequence and query head to its output, in their order.
+// The chunks of a sequence and query head to its output, in their order.
 template <typename T, int D>
-__global__ void __launch_bounds__(256) swa_paged_join_kernel(PagedArgs a)
+__global__ void __launch_bounds__(256) swa_paged_join_chunks_kernel(PagedArgs a)
 {
-    constexpr int kLanes = D / 4, kShares = 256 / kLanes;
-    const int s = blockIdx.x / a.h_q, hq = blockIdx.x - s * a.h_q, tid = threadIdx.x, share = tid / kLanes, c = (tid % kLanes) * 4;
+    constexpr int kLanes = D / 4, kTeams = 256 / kLanes;
+    const int s = blockIdx.x / a.h_q, hq = blockIdx.x - s * a.h_q, tid = threadIdx.x, team = tid / kLanes, lane = tid % kLanes;
     int row, lo, n;
     bool too_long;
-    if (!paged_sequence(a, s, row, lo, n, too_long)) return;
-    const int base0 = lo & ~31, chunks = n > base0 ? (n - base0 + a.chunk - 1) / a.chunk : 1;
-    if (chunks == 1) return;
-    const int64_t at = ((int64_t)s * a.h_q + hq) * a.splits;
-    __shared__ float weight[kPagedMaxSplits], waves[4], waves2[4];
-    __shared__ f32x4_t part[kShares][kLanes];
-    const float2 mine = tid < chunks ? *reinterpret_cast<const float2*>(a.part_sum + (at + tid) * 2) : float2{-INFINITY, 0.f};
+    if (!paged_sequence(a, s, row, lo, n, too_long) || n - (lo & ~31) <= a.chunk) return;
+    const int count = (n - (lo & ~31) + a.chunk - 1) / a.chunk, kv = hq / a.group, of = hq - kv * a.group;
+    const int64_t stride = a.row_tiles * a.heads, first = ((int64_t)s * a.h_kv + kv) * a.ranges * stride + (of >> 4) * a.heads + (of & 15);
+    __shared__ float weight[kPagedChunks], waves[4], waves2[4];
+    __shared__ f32x4_t part[kTeams][kLanes];
+    const float2 mine = tid < count ? *reinterpret_cast<const float2*>(a.part_sum + (first + tid * stride) * 2) : float2{-INFINITY, 0.f};
     float top = wave_max(mine.x);
     if ((tid & 63) == 0) waves[tid >> 6] = top;
     __syncthreads();
@@ -363,17 +539,85 @@ __global__ void __launch_bounds__(256) swa_paged_join_kernel(PagedArgs a)
     const float total = (waves2[0] + waves2[1]) + (waves2[2] + waves2[3]);
     f32x4_t y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-    for (int i = share; i < chunks; i += kShares) y += *reinterpret_cast<const f32x4_t*>(a.part_out + (at + i) * D + c) * weight[i];
-    part[share][tid % kLanes] = y;
+    for (int i = team; i < count; i += kTeams) y += *reinterpret_cast<const f32x4_t*>(a.part_out + (first + i * stride) * D + lane * 4) * weight[i];
+    part[team][lane] = y;
     __syncthreads();
-    if (share) return;
+    if (team) return;
 #pragma unroll
-    for (int i = 1; i < kShares; ++i) y += part[i][tid];
-    char* const to = a.out + ((int64_t)row * a.h_q + hq) * (D * Elem<T>::kBytes);
+    for (int i = 1; i < kTeams; ++i) y += part[i][lane];
+    const int64_t to = (int64_t)row * a.h_q + hq;
     const float inverse = 1.f / total;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) store_elem<T>(to, c + i, total == 0.f ? 0.f : y[i] * inverse);
-    if (a.lse && tid == 0) a.lse[(int64_t)row * a.h_q + hq] = (top + __builtin_log2f(total)) * 0.69314718055994530942f;
+    for (int i = 0; i < 4; ++i) store_elem<T>(a.out + to * (D * Elem<T>::kBytes), lane * 4 + i, total == 0.f ? 0.f : y[i] * inverse);
+    if (a.lse && lane == 0) a.lse[to] = (top + __builtin_log2f(total)) * 0.69314718055994530942f;
+}
+
+// The pieces of the sequence that a share begins and does not end, likewise; a workgroup has `per` of its query heads, a power of two.
+template <typename T, int D>
+__global__ void __launch_bounds__(256) swa_paged_join_shares_kernel(PagedArgs a, int per)
+{
+    constexpr int kLanes = D / 4, kTeams = 256 / kLanes;
+    const int blocks = (a.heads + per - 1) / per, share = blockIdx.x / (a.row_tiles * blocks), rest = blockIdx.x - share * a.row_tiles * blocks;
+    const int4 unit = a.begun[share];
+    if (unit.x == 0) return;
+    const int kv = unit.x - 1, row = unit.y, count = unit.z, tile = rest / blocks, tid = threadIdx.x, team = tid / kLanes, lane = tid % kLanes,
+              mates = kTeams / per, mate = team % mates, head = (rest - tile * blocks) * per + team / mates;
+    const bool there = head < a.heads && 16 * tile + head < a.group;
+    // the share's second piece, and then the first ones of the shares behind it
+    auto at = [&](int i) { return ((int64_t)(2 * (share + i) + (i == 0)) * a.row_tiles + tile) * a.heads + head; };
+    float top = -INFINITY;
+    if (there)
+        for (int i = mate * kLanes + lane; i < count; i += mates * kLanes) top = fmaxf(top, a.part_sum[at(i) * 2]);
+#pragma unroll
+    for (int o = 1; o < kLanes; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    __shared__ float tops[kTeams], sums[kTeams];
+    __shared__ f32x4_t part[kTeams][kLanes];
+    if (lane == 0) tops[team] = top;
+    __syncthreads();
+    for (int i = 0; i < mates; ++i) top = fmaxf(top, tops[team - mate + i]);
+    const float from = top == -INFINITY ? 0.f : top;
+    f32x4_t y = {0.f, 0.f, 0.f, 0.f};
+    float total = 0.f;
+    if (there) {
+#pragma unroll 4
+        for (int i = mate; i < count; i += mates) {
+            const float2 m = *reinterpret_cast<const float2*>(a.part_sum + at(i) * 2);
+            const float w = __builtin_amdgcn_exp2f(m.x - from);
+            y += *reinterpret_cast<const f32x4_t*>(a.part_out + at(i) * D + lane * 4) * w;
+            total = __builtin_fmaf(m.y, w, total);
+        }
+    }
+    part[team][lane] = y;
+    if (lane == 0) sums[team] = total;
+    __syncthreads();
+    if (mate || !there) return;
+    for (int i = 1; i < mates; ++i) {
+        y += part[team + i][lane];
+        total += sums[team + i];
+    }
+    const int64_t to = (int64_t)row * a.h_q + (int64_t)kv * a.group + 16 * tile + head;
+    const float inverse = 1.f / total;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) store_elem<T>(a.out + to * (D * Elem<T>::kBytes), lane * 4 + i, total == 0.f ? 0.f : y[i] * inverse);
+    if (a.lse && lane == 0) a.lse[to] = (top + __builtin_log2f(total)) * 0.69314718055994530942f;
+}
+
+template <typename T, typename C, int D>
+static void launch_paged_form(const PagedArgs& a, bool in_shares, hipStream_t stream)
+{
+    const int64_t units = (int64_t)a.b * a.h_kv, works = (in_shares ? a.ranges : units * a.ranges);
+    const dim3 grid((unsigned)((works + 7) / 8 * 8 * a.row_tiles)), block(64 * kPagedWaves);
+    if (in_shares) launch_kernel(swa_paged_decode_kernel<T, C, D, true>, grid, block, sizeof(int) * ((size_t)a.b + 1), stream, a);
+    else launch_kernel(swa_paged_decode_kernel<T, C, D, false>, grid, block, 0, stream, a);
+    if (a.ranges == 1) return;
+    if (!in_shares) {
+        launch_kernel(swa_paged_join_chunks_kernel<T, D>, dim3((unsigned)((int64_t)a.b * a.h_q)), dim3(256), 0, stream, a);
+        return;
+    }
+    int per = 1;                                         // (few pieces of a sequence: a workgroup joins several heads)
+    while (per < 1024 / D && per < a.heads) per *= 2;
+    launch_kernel(swa_paged_join_shares_kernel<T, D>, dim3((unsigned)((int64_t)a.ranges * a.row_tiles * ((a.heads + per - 1) / per))), dim3(256), 0,
+                  stream, a, per);
 }
 
 int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_rows, const int32_t* row_start, const void* k_pages,
@@ -410,37 +654,31 @@ int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_
     while ((1 << l) < p.page_size) ++l;
     a.page_shift = 31 + l;
     a.page_mul = (uint32_t)(((UINT64_C(1) << a.page_shift) + p.page_size - 1) / p.page_size);
+    a.sixteens = p.page_size % 16 == 0;
     a.scale = (p.scale > 0.f ? p.scale : 1.f / sqrtf((float)p.d)) * 1.44269504088896340736f;
 
     const int64_t units = (int64_t)p.b * p.h_kv;
-    const int step = kPagedWaves * 32;
-    const int64_t span = p.window > 0 && p.window < a.len_max ? (int64_t)p.window + 31 : a.len_max;
-    int64_t splits = paged_max_splits(p);
-    if (splits > (span + step - 1) / step) splits = (span + step - 1) / step;
-    a.chunk = (int32_t)(((span + splits - 1) / splits + step - 1) / step * step);
-    a.splits = (int32_t)((span + a.chunk - 1) / a.chunk);
+    const int64_t span = paged_span(p);
+    const int64_t steps = units * ((span + kPagedStep - 1) / kPagedStep);
+    if (steps > 0x7fffffffLL) return SWA_ERR_CAPACITY;
+    a.heads = a.group < 16 ? a.group : 16;
+    const bool in_shares = paged_in_shares(p);
+    if (in_shares) {
+        a.ranges = paged_max_shares(p);
+    } else {
+        const int64_t of_one = steps / units, each = (of_one + paged_max_chunks(p) - 1) / paged_max_chunks(p);
+        a.chunk = (int32_t)(each * kPagedStep);
+        a.ranges = (int32_t)((of_one + each - 1) / each);
+    }
     a.part_out = reinterpret_cast<float*>(static_cast<char*>(workspace) + kPagedPartialOffset);
-    a.part_sum = a.part_out + (int64_t)p.b * p.h_q * a.splits * p.d;
+    a.part_sum = a.part_out + paged_piece_rows(p) * p.d;
+    a.begun = reinterpret_cast<int4*>(a.part_sum + paged_piece_rows(p) * 2);
 
-    const int64_t works = (units * a.splits + 7) / 8 * 8;
-    if (works * a.row_tiles > 0x7fffffffLL) return SWA_ERR_BAD_SHAPE;
-    const dim3 grid((unsigned)(works * a.row_tiles)), block(64 * kPagedWaves);
-#define SWA_PAGED(T, C) \
-    (p.d == 64 ? launch_kernel(swa_paged_decode_kernel<T, C, 64>, grid, block, 0, stream, a) \
-               : launch_kernel(swa_paged_decode_kernel<T, C, 128>, grid, block, 0, stream, a))
+#define SWA_PAGED(T, C) (p.d == 64 ? launch_paged_form<T, C, 64>(a, in_shares, stream) : launch_paged_form<T, C, 128>(a, in_shares, stream))
     if (p.dtype == SWA_F32) SWA_PAGED(F32, F32);
     else if (p.dtype == SWA_F16) paged_int8(p) ? SWA_PAGED(F16, Q8) : SWA_PAGED(F16, F16);
     else paged_int8(p) ? SWA_PAGED(BF16, Q8) : SWA_PAGED(BF16, BF16);
 #undef SWA_PAGED
-    if (a.splits > 1) {
-        const dim3 join((unsigned)((int64_t)p.b * p.h_q));
-#define SWA_JOIN(T) (p.d == 64 ? launch_kernel(swa_paged_join_kernel<T, 64>, join, dim3(256), 0, stream, a) \
-                               : launch_kernel(swa_paged_join_kernel<T, 128>, join, dim3(256), 0, stream, a))
-        if (p.dtype == SWA_F32) SWA_JOIN(F32);
-        else if (p.dtype == SWA_F16) SWA_JOIN(F16);
-        else SWA_JOIN(BF16);
-#undef SWA_JOIN
-    }
     return hipGetLastError() == hipSuccess ? SWA_OK : SWA_ERR_HIP;
 }
 
