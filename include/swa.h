@@ -526,7 +526,7 @@ int swa_paged_plan(const swa_paged_params *params, const int32_t *new_cnt, const
  * q_out gets the queries, slot[r] of k_pages and v_pages the keys and the values as they came.  All in fp32, the angle in
  * fp64 until it is reduced to one turn; rounded once.  With SWA_KV_INT8 a row is stored as scale = max |x| / 127 and codes
  * round(x / scale), ties to even (zeros where scale is below 2^-126); a row with a value that is not finite reads back as NaN.
- * A row with a negative slot is left out: nothing is read or written for it.  A slot outside the pool is left out too and
+ * A row with a negative slot is left out: nothing is written for it.  A slot outside the pool is left out too and
  * sets the SWA_ERR_BAD_REQUEST bit.  The slots of one call are distinct (as swa_paged_plan makes them): of two rows with the
  * same slot either may end up in it, or some heads of each.
  *   q [n_rows, h_q, d], k, v [n_rows, h_kv, d] (in); pos [axes, n_rows] int32; slot [n_rows]; inv_freq [rot_dim/2] float32

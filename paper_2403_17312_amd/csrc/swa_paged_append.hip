@@ -3,9 +3,11 @@
 //
 // D / 8 lanes hold one head's row, 8 channels each, so a wave has 64 / (D / 8) heads in hand: the norm's sum is a DPP reduction over those
 // lanes, and the other channel of a rotated pair, rot_dim / 2 channels on, is at the same place of another lane (or, for
-// neighbouring pairs, in the same lane).  The angles depend on row and channel alone: a lane forms its own sines and cosines once and
-// keeps them for all heads of the row.  An angle of a far position has no digits left in fp32 (position 10^6: 0.06), so
-// position * inv_freq / 2 pi is an fp64 product, whose whole turns go before it is rounded.
+// neighbouring pairs, in the same lane).  A wave takes one row's queries, keys and values in turn, a wave's heads of one kind at a time, with the
+// next ones' loads under way.  The angles depend on row and channel alone: a lane forms its own sines and cosines once for all
+// heads of the row, and with the norm's weights makes two factors of them, y = (x_i a_i + x_j b_i) / rms.  An angle of a far position has no
+// digits left in fp32 (position 10^6: 0.06), so position * inv_freq / 2 pi is an fp64 product, whose whole turns go before it is rounded;
+// the hardware's sine and cosine of a turn are within 2^-22.9 (all of [-1/2, 1/2], in steps of 2^-24).
 #include <type_traits>
 
 #include "swa_paged.hpp"
@@ -39,10 +41,14 @@ struct Raw8 {
 #pragma unroll
         for (int i = 0; i < Elem<T>::kBytes / 2; ++i) v[i] = load16(p + 16 * i);
     }
+    template <bool STREAM>
     __device__ __forceinline__ void store(char* p) const
     {
 #pragma unroll
-        for (int i = 0; i < Elem<T>::kBytes / 2; ++i) store16(p + 16 * i, v[i]);
+        for (int i = 0; i < Elem<T>::kBytes / 2; ++i) {
+            if constexpr (STREAM) __builtin_nontemporal_store(__builtin_bit_cast(u32x4_t, v[i]), reinterpret_cast<u32x4_t*>(p + 16 * i));
+            else store16(p + 16 * i, v[i]);
+        }
     }
     __device__ __forceinline__ void widen(float* f) const
     {
@@ -86,15 +92,43 @@ __device__ __forceinline__ uint32_t group_max_bits(uint32_t v)
     return v;
 }
 
-template <typename T, int D, bool INT8, bool NEIGHBOURS>
+// A lane's channels of the heads of one pass.
+template <typename T, int D>
+__device__ __forceinline__ void fetch_heads(Raw8<T>& raw, const AppendArgs& a, int row, int pass, int q_passes, int kv_passes, int mine, int sub)
+{
+    constexpr int kHeads = 512 / D;
+    const char* from = a.q + row * a.q_stride;
+    int first = 0, heads = a.h_q;
+    if (pass >= q_passes) {
+        from = a.k + row * a.k_stride;
+        first = q_passes;
+        heads = a.h_kv;
+    }
+    if (pass >= q_passes + kv_passes) {
+        from = a.v + row * a.v_stride;
+        first = q_passes + kv_passes;
+    }
+    const int head = (pass - first) * kHeads + mine;
+    raw = Raw8<T>{};
+    if (head < heads) raw.load(from + (uint32_t)((head * D + 8 * sub) * Elem<T>::kBytes));
+}
+
+// STREAM: rows are stored past the caches.
+template <typename T, int D, bool INT8, bool NEIGHBOURS, bool STREAM>
 __global__ void __launch_bounds__(kAppendThreads) swa_paged_append_kernel(AppendArgs a)
 {
-    constexpr int kLanes = D / 8, kHeads = 64 / kLanes;
+    constexpr int kLanes = D / 8, kHeads = 64 / kLanes, kRow = D * Elem<T>::kBytes, kLane = 8 * Elem<T>::kBytes;
     const int lane = threadIdx.x & 63, sub = lane % kLanes, mine = lane / kLanes;
     const int64_t wave = (int64_t)blockIdx.x * (kAppendThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t row64 = wave >> a.log_parts;
     if (row64 >= a.n_rows) return;
     const int row = (int)row64, part = (int)(wave & ((1 << a.log_parts) - 1));
+
+    // Passes: kHeads queries each, then kHeads keys, then values.
+    const int q_passes = (a.h_q + kHeads - 1) / kHeads, kv_passes = (a.h_kv + kHeads - 1) / kHeads, passes = q_passes + 2 * kv_passes;
+    if (part >= passes) return;
+    Raw8<T> next;
+    fetch_heads<T, D>(next, a, row, part, q_passes, kv_passes, mine, sub);
     const int32_t slot = a.slot[row];
     if (slot < 0) return;
     if (slot >= a.total_slots) {
@@ -102,6 +136,7 @@ __global__ void __launch_bounds__(kAppendThreads) swa_paged_append_kernel(Append
         return;
     }
     const int32_t page = slot / a.page_size, off = slot - page * a.page_size;
+    const int64_t kv_row = (int64_t)page * a.h_kv * a.page_size + off;      // of key head 0
 
     // this lane's channels 8 sub .. 8 sub + 7: x <- x c + other s
     const int half = a.rot_dim / 16;               // lanes of half the rotated channels
@@ -117,97 +152,109 @@ __global__ void __launch_bounds__(kAppendThreads) swa_paged_append_kernel(Append
         }
         c[i] = 1.f;
         s[i] = 0.f;
-        if (turns) {
+        if (turns && part < q_passes + kv_passes) {
             const int pair = NEIGHBOURS ? 4 * sub + i / 2 : 8 * (sub < half ? sub : sub - half) + i;
             int axis = 0;
 #pragma unroll
             for (int x = 0; x + 1 < SWA_MAX_ROPE_AXES; ++x) axis += pair >= a.axis_end[x];
             const double turn = (double)a.pos[(int64_t)axis * a.n_rows + row] * (double)a.inv_freq[pair] * 0.15915494309189533577;
-            sincospif(2.f * (float)(turn - __builtin_rint(turn)), &s[i], &c[i]);
+            const float rest = (float)(turn - __builtin_rint(turn));
+            s[i] = __builtin_amdgcn_sinf(rest);
+            c[i] = __builtin_amdgcn_cosf(rest);
             if (NEIGHBOURS || sub < half) s[i] = -s[i];
         }
     }
 
-    const int heads = a.h_q + 2 * a.h_kv;
-    for (int h0 = part * kHeads; h0 < heads; h0 += kHeads << a.log_parts) {
-        const int head = h0 + mine;
-        const bool there = head < heads, is_q = head < a.h_q, is_v = head >= a.h_q + a.h_kv;
-        const int kv_head = is_v ? head - a.h_q - a.h_kv : head - a.h_q;
-        const char* const src = is_q ? a.q + row * a.q_stride + (int64_t)head * (D * Elem<T>::kBytes)
-                                : (is_v ? a.v + row * a.v_stride : a.k + row * a.k_stride) + (int64_t)kv_head * (D * Elem<T>::kBytes);
-        Raw8<T> raw{};
-        if (there) raw.load(src + 8 * Elem<T>::kBytes * sub);
-        float x[8], y[8];
+    float own[8], cross[8];                        // what a channel and the other one of its pair are multiplied by, weights included
+    int weighed = -1;                              // for queries (0) or keys (1)
+    for (int pass = part; pass < passes; pass += 1 << a.log_parts) {
+        Raw8<T> raw = next;
+        if (pass + (1 << a.log_parts) < passes) fetch_heads<T, D>(next, a, row, pass + (1 << a.log_parts), q_passes, kv_passes, mine, sub);
+        const bool is_q = pass < q_passes, is_v = pass >= q_passes + kv_passes;
+        const int head = (pass - (is_v ? q_passes + kv_passes : is_q ? 0 : q_passes)) * kHeads + mine;
+        const bool there = head < (is_q ? a.h_q : a.h_kv);
+        const int64_t to_row = is_q ? (int64_t)row * a.h_q + head : kv_row + (int64_t)head * a.page_size;
+        if (is_v && !INT8) {
+            if (there) raw.template store<STREAM>(a.v_pages + to_row * kRow + sub * kLane);
+            continue;
+        }
+        float x[8];
         raw.widen(x);
-        const char* const weight = is_v ? nullptr : is_q ? a.q_weight : a.k_weight;
-        float square = 0.f;
+        if (!is_v) {
+            const char* const weight = is_q ? a.q_weight : a.k_weight;
+            if (weighed != (is_q ? 0 : 1)) {
+                weighed = is_q ? 0 : 1;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) square = __builtin_fmaf(x[i], x[i], square);
-        square = group_sum<kLanes>(square);
-        const float norm = weight ? 1.f / sqrtf(square * (1.f / D) + a.eps) : 1.f;
-        const Raw8<T> raw2 = NEIGHBOURS ? raw : raw.from_lane(mine * kLanes + other);
-        raw2.widen(y);
-        if (weight) {
-            float w[8];
-            Raw8<T> rw;
-            rw.load(weight + 8 * Elem<T>::kBytes * sub);
-            rw.widen(w);
+                for (int i = 0; i < 8; ++i) {
+                    own[i] = c[i];
+                    cross[i] = s[i];
+                }
+                if (weight) {
+                    Raw8<T> w, w_other;
+                    w.load(weight + sub * kLane);
+                    w_other.load(weight + other * kLane);
+                    float f[8], g[8];
+                    w.widen(f);
+                    w_other.widen(g);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = x[i] * norm * w[i];
-            if (!NEIGHBOURS) {
-                rw.load(weight + 8 * Elem<T>::kBytes * other);
-                rw.widen(w);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = y[i] * norm * w[i];
+                    for (int i = 0; i < 8; ++i) {
+                        own[i] *= f[i];
+                        cross[i] *= g[NEIGHBOURS ? i ^ 1 : i];
+                    }
+                }
             }
-        }
-        if (NEIGHBOURS) {
+            float norm = 1.f;
+            if (weight) {
+                float square = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = x[i ^ 1];
-        }
-        if (turns && !is_v) {
+                for (int i = 0; i < 8; ++i) square = __builtin_fmaf(x[i], x[i], square);
+                norm = __builtin_amdgcn_rsqf(group_sum<kLanes>(square) * (1.f / D) + a.eps);
+            }
+            float y[8], z[8];
+            if (!NEIGHBOURS) raw.from_lane(mine * kLanes + other).widen(y);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = x[i] * c[i] + y[i] * s[i];
+            for (int i = 0; i < 8; ++i) {
+                const float t = x[i] * own[i];
+                z[i] = (turns ? __builtin_fmaf(NEIGHBOURS ? x[i ^ 1] : y[i], cross[i], t) : t) * norm;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = z[i];
         }
         if (!INT8 || is_q) {
             raw.round(x);
-            char* const dst = is_q ? a.q_out + ((int64_t)row * a.h_q + head) * (D * Elem<T>::kBytes)
-                                   : (is_v ? a.v_pages : a.k_pages) +
-                                         (((int64_t)page * a.h_kv + kv_head) * a.page_size + off) * (D * Elem<T>::kBytes);
-            if (there) raw.store(dst + 8 * Elem<T>::kBytes * sub);
+            if (there) raw.template store<STREAM>((is_q ? a.q_out : a.k_pages) + to_row * kRow + sub * kLane);
+            continue;
         }
-        if (INT8) {
-            uint32_t top = 0;
+        uint32_t top = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t m = f2u(x[i]) & 0x7fffffffu;
-                top = m > top ? m : top;
-            }
-            // rows below 2^-119 have no scale with a reciprocal in fp32: their codes are 0
-            const float scale = u2f(group_max_bits<kLanes>(top)) * (1.f / 127.f);
-            const bool tiny = scale < 1.17549435e-38f;
-            const float inverse = tiny ? 0.f : 1.f / scale;
-            uint32_t codes[2] = {0u, 0u};
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t m = f2u(x[i]) & 0x7fffffffu;
+            top = m > top ? m : top;
+        }
+        // (rows below 2^-119 have no scale with a reciprocal in fp32: their codes are 0)
+        top = group_max_bits<kLanes>(top);
+        const float scale = u2f(top < 0x7f800000u ? top : 0x7fc00000u) * (1.f / 127.f);
+        const bool tiny = scale < 1.17549435e-38f;
+        const float inverse = tiny ? 0.f : __builtin_amdgcn_rcpf(scale);
+        uint32_t codes[2] = {0u, 0u};
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float t = rintf(x[i] * inverse);
-                t = t < -127.f ? -127.f : (t > 127.f ? 127.f : t);
-                codes[i / 4] |= ((uint32_t)(int32_t)t & 0xffu) << (8 * (i % 4));
-            }
-            if (there && !is_q) {
-                const int64_t r = ((int64_t)page * a.h_kv + kv_head) * a.page_size + off;
-                *reinterpret_cast<uint2*>((is_v ? a.v_pages : a.k_pages) + r * D + 8 * sub) = uint2{codes[0], codes[1]};
-                if (sub == 0) (is_v ? a.v_scale : a.k_scale)[r] = tiny ? 0.f : scale;
-            }
+        for (int i = 0; i < 8; ++i) {
+            const float t = fminf(fmaxf(rintf(x[i] * inverse), -127.f), 127.f);
+            codes[i / 4] |= ((uint32_t)(int32_t)t & 0xffu) << (8 * (i % 4));
+        }
+        if (there) {
+            *reinterpret_cast<uint2*>((is_v ? a.v_pages : a.k_pages) + to_row * D + 8 * sub) = uint2{codes[0], codes[1]};
+            if (sub == 0) (is_v ? a.v_scale : a.k_scale)[to_row] = tiny ? 0.f : scale;
         }
     }
 }
 
 template <typename T, int D, bool INT8>
-static void launch_append_form(const AppendArgs& a, bool neighbours, dim3 grid, hipStream_t stream)
+static void launch_append_form(const AppendArgs& a, bool neighbours, bool past, dim3 grid, hipStream_t stream)
 {
-    launch_kernel(neighbours ? swa_paged_append_kernel<T, D, INT8, true> : swa_paged_append_kernel<T, D, INT8, false>, grid, dim3(kAppendThreads), 0,
-                  stream, a);
+    auto kernel = neighbours ? (past ? swa_paged_append_kernel<T, D, INT8, true, true> : swa_paged_append_kernel<T, D, INT8, true, false>)
+                             : (past ? swa_paged_append_kernel<T, D, INT8, false, true> : swa_paged_append_kernel<T, D, INT8, false, false>);
+    launch_kernel(kernel, grid, dim3(kAppendThreads), 0, stream, a);
 }
 
 int launch_paged_append(const swa_paged_params& p, const swa_rows& q, const swa_rows& k, const swa_rows& v, int32_t n_rows, const int32_t* pos,
@@ -245,14 +292,21 @@ int launch_paged_append(const swa_paged_params& p, const swa_rows& q, const swa_
         a.axis_end[i] = i + 1 < p.axes ? end : INT32_MAX;
     }
     a.eps = p.eps;
-    // a row's heads are shared out while that leaves waves to fill the chip with
-    const int passes = (p.h_q + 2 * p.h_kv + 64 / (p.d / 8) - 1) / (64 / (p.d / 8));
-    while ((2 << a.log_parts) <= passes && ((int64_t)n_rows << a.log_parts) < 4096) ++a.log_parts;
+    // A row's passes are shared out among waves until there are 2048, and further while they are many: us with 1 / 2 / 4 / 8 waves a row, 32 query and 8 key
+    // heads of 128 bf16 channels (12 passes): 512 rows - / - / 7.0 / 7.8, 1024 - / 8.9 / 8.9 / 11.1, 2048 13.1 / 12.3 / 13.0 / -, 4096 19.3 / 21.0; 64 and 8 heads, fp16
+    // into codes (20 passes), 8192 rows 92 / 82.
+    const int of_wave = 64 / (p.d / 8), passes = (p.h_q + of_wave - 1) / of_wave + 2 * ((p.h_kv + of_wave - 1) / of_wave);
+    auto more = [&](int64_t waves, int each) { return waves < 2048 || (waves <= 2048 && each >= 12) || (waves <= 8192 && each >= 16); };
+    while ((1 << a.log_parts) < passes && more((int64_t)n_rows << a.log_parts, passes >> a.log_parts)) ++a.log_parts;
+    // Many rows fill the caches with what nothing reads soon: 4096 rows as above 26.6 us stored through them, 19.3 past them; 8192 rows 49.5, 44.5 (4.5
+    // TB/s); 256 rows and the attention behind them 47.1, 45.7.  Of few, the attention finds queries and keys there: 1 row and 100 tokens 8.7, 9.0.  (Not in fp32, where a lane
+    // stores a row's bytes in two halves, which meet in a cache: 1001 rows of 32 and 32 heads, d = 64, 11.0, 11.75.)
+    const bool past = bytes == 2 && (int64_t)n_rows * (p.h_q + 2 * p.h_kv) * p.d * bytes >= (2 << 20);
     const int64_t waves = (int64_t)n_rows << a.log_parts;
     const dim3 grid((unsigned)((waves + kAppendThreads / 64 - 1) / (kAppendThreads / 64)));
     const bool neighbours = (p.flags & SWA_ROPE_INTERLEAVED) != 0;
 #define SWA_APPEND(T, INT8) \
-    (p.d == 64 ? launch_append_form<T, 64, INT8>(a, neighbours, grid, stream) : launch_append_form<T, 128, INT8>(a, neighbours, grid, stream))
+    (p.d == 64 ? launch_append_form<T, 64, INT8>(a, neighbours, past, grid, stream) : launch_append_form<T, 128, INT8>(a, neighbours, past, grid, stream))
     if (p.dtype == SWA_F32) SWA_APPEND(F32, false);
     else if (p.dtype == SWA_F16) paged_int8(p) ? SWA_APPEND(F16, true) : SWA_APPEND(F16, false);
     else paged_int8(p) ? SWA_APPEND(BF16, true) : SWA_APPEND(BF16, false);
