@@ -299,9 +299,8 @@ int launch_paged_append(const swa_paged_params& p, const swa_rows& q, const swa_
     auto more = [&](int64_t waves, int each) { return waves < 2048 || (waves <= 2048 && each >= 12) || (waves <= 8192 && each >= 16); };
     while ((1 << a.log_parts) < passes && more((int64_t)n_rows << a.log_parts, passes >> a.log_parts)) ++a.log_parts;
     // Many rows fill the caches with what nothing reads soon: 4096 rows as above 26.6 us stored through them, 19.3 past them; 8192 rows 49.5, 44.5 (4.5
-    // TB/s); 256 rows and the attention behind them 47.1, 45.7.  Of few, the attention finds queries and keys there: 1 row and 100 tokens 8.7, 9.0.  (Not in fp32, where a lane
-    // stores a row's bytes in two halves, which meet in a cache: 1001 rows of 32 and 32 heads, d = 64, 11.0, 11.75.)
-    const bool past = bytes == 2 && (int64_t)n_rows * (p.h_q + 2 * p.h_kv) * p.d * bytes >= (2 << 20);
+    // TB/s); 256 rows and the attention behind them 47.1, 45.7.  Of few, the attention finds queries and keys there: 1 row and 100 tokens 8.7, 9.0.
+    const bool past = (int64_t)n_rows * (p.h_q + 2 * p.h_kv) * p.d * bytes >= (2 << 20);
     const int64_t waves = (int64_t)n_rows << a.log_parts;
     const dim3 grid((unsigned)((waves + kAppendThreads / 64 - 1) / (kAppendThreads / 64)));
     const bool neighbours = (p.flags & SWA_ROPE_INTERLEAVED) != 0;
