@@ -15,6 +15,16 @@ inline int paged_row_bytes(const swa_paged_params& p) { return paged_int8(p) ? p
 
 inline int32_t* paged_status(void* workspace) { return reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + kWsStatusOffset); }
 
+// t / page_size as (t * mul) >> shift, exact for 0 <= t < 2^31: with 2^(l-1) < page_size <= 2^l, mul = ceil(2^(31 + l) / page_size) is below 2^32, and it is
+// too large by less than one, which t times over stays below 2^31 <= 2^(31 + l) / page_size, the step to the next quotient.
+inline void page_divisor(int32_t page_size, uint32_t& mul, int32_t& shift)
+{
+    int l = 0;
+    while ((1 << l) < page_size) ++l;
+    shift = 31 + l;
+    mul = (uint32_t)(((UINT64_C(1) << shift) + page_size - 1) / page_size);
+}
+
 constexpr size_t kPagedPartialOffset = 256;    // the status word lies before the attention's partial results
 
 // Bytes of the partial results of swa_paged_decode, for any len_bound and window.

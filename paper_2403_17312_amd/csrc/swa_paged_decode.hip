@@ -649,11 +649,7 @@ int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_
     if (p.len_bound > 0 && p.len_bound < a.len_max) a.len_max = p.len_bound;
     a.group = p.h_q / p.h_kv;
     a.row_tiles = (a.group + 15) / 16;
-    // exact for numerators below 2^31: the error of page_mul, below page_size <= 2^l, times the numerator stays below 2^(31 + l)
-    int l = 0;
-    while ((1 << l) < p.page_size) ++l;
-    a.page_shift = 31 + l;
-    a.page_mul = (uint32_t)(((UINT64_C(1) << a.page_shift) + p.page_size - 1) / p.page_size);
+    page_divisor(p.page_size, a.page_mul, a.page_shift);
     a.sixteens = p.page_size % 16 == 0;
     a.scale = (p.scale > 0.f ? p.scale : 1.f / sqrtf((float)p.d)) * 1.44269504088896340736f;
 
