@@ -472,7 +472,7 @@ typedef struct {
     int32_t dtype;      /* swa_dtype of q, k, v, weights, out, and of the pages without SWA_KV_INT8 */
     float scale;        /* logit scale; 0 selects 1/sqrt(d) */
     int32_t window;     /* 0, or how many of the last tokens the attention sees */
-    int32_t len_bound;  /* 0, or an upper bound on cache_len for swa_paged_decode, which it sizes its launch to */
+    int32_t len_bound;  /* 0, or an upper bound on cache_len for swa_paged_decode, which sizes its launch to it */
     int32_t flags;
     int32_t rot_dim;    /* channels that the rotation takes, the first ones of a row: a multiple of 16, 0..d */
     int32_t axes;       /* position axes, 1..SWA_MAX_ROPE_AXES */

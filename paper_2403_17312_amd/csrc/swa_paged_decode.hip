@@ -3,7 +3,7 @@
 //
 // A workgroup serves up to 16 of the query heads that share a key head, over a range of one sequence's tokens; its four waves take tiles of the range
 // in turn, each with a running maximum and sum of the softmax.  Ranges come in two ways:
-//   chunks   few sequences: each one's tokens in equal chunks, as many as the bound on the lengths gives, a workgroup for each.
+//   chunks   few sequences: each one's tokens in equal chunks, as many as fill the CUs evenly, a workgroup for each.
 //   shares   many, and long ones: the call's work, in steps of 128 tokens of one sequence and key head, laid end to end and cut into as
 //            many equal shares as there are workgroups, whatever the lengths are; each workgroup sums the lengths up by itself.  A share
 //            holds whole sequences and at most two pieces.  128 sequences of 512 to 8192 tokens, 8 key heads of 128 bf16 channels: chunks 425 us, shares 353 (6.5 TB/s).
@@ -38,7 +38,7 @@ struct PagedArgs {
     int32_t b, n_rows, h_q, h_kv, page_size, n_pages, max_pages, window, len_max;
     int32_t group, row_tiles, heads;               // query heads of a key head, tiles of 16 of them, heads of a tile at most
     int32_t ranges;                                // shares, or chunks of a sequence at most
-    int32_t chunk;                                 // tokens
+    int32_t chunk;                                 // tokens; 0: the longest sequence says
     uint32_t page_mul;                             // t / page_size = t * page_mul >> page_shift for 0 <= t < 2^31
     int32_t page_shift;
     int32_t sixteens;                              // pages are whole sixteens of tokens
@@ -80,11 +80,11 @@ static int paged_max_shares(const swa_paged_params& p)
     return n < 1 ? 1 : n;
 }
 
-// Chunks of a sequence at most.
-static int paged_max_chunks(const swa_paged_params& p)
+// Chunks of a sequence at most, for k workgroups on every CU.
+static int paged_chunks(const swa_paged_params& p, int k)
 {
-    const int64_t n = (1024 + paged_units(p) - 1) / paged_units(p);
-    return n > kPagedChunks ? kPagedChunks : (int)n;
+    const int64_t n = 256 * k / paged_units(p);
+    return n < 1 ? 1 : n > kPagedChunks ? kPagedChunks : (int)n;
 }
 
 // (for either form, whatever length and window a call states)
@@ -92,7 +92,7 @@ static int64_t paged_piece_rows(const swa_paged_params& p)
 {
     const int group = p.h_q / p.h_kv;
     const int64_t shares = 2 * (int64_t)paged_max_shares(p) * row_tiles_of(p);
-    const int64_t chunks = paged_max_chunks(p) > 1 ? paged_max_chunks(p) * paged_units(p) : 0;
+    const int64_t chunks = paged_chunks(p, 3) > 1 ? paged_chunks(p, 3) * paged_units(p) : 0;
     const int64_t pieces = paged_units(p) >= 64 && shares > chunks ? shares : chunks;
     return 2 * ((pieces * (group < 16 ? group : 16) + 1) / 2);
 }
@@ -153,6 +153,24 @@ __device__ __forceinline__ int paged_sequence(const PagedArgs& a, int s, int& ro
     lo = a.window && n > a.window ? n - a.window : 0;
     const int tokens = n - (lo & ~31);                   // (tiles begin at multiples of 32)
     return tokens > kPagedStep ? (tokens + kPagedStep - 1) / kPagedStep : 1;
+}
+
+// Tokens of a chunk: a sequence has a.ranges chunks at most.  Where the caller states no bound, a table may be far wider than the lengths, and the longest of
+// those says (a microsecond of every call; 64 sequences, a wave's lanes, at most).
+__device__ __forceinline__ int paged_chunk(const PagedArgs& a)
+{
+    if (a.chunk) return a.chunk;
+    const int lane = threadIdx.x & 63;
+    int row, lo = 0, n = 0, tokens = 1;
+    bool too_long = false;
+    if (lane < a.b && paged_sequence(a, lane, row, lo, n, too_long)) tokens = n - (lo & ~31);
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+        const int other = __shfl_xor(tokens, o, 64);
+        tokens = tokens > other ? tokens : other;
+    }
+    const int per_step = a.ranges * kPagedStep;          // (at most 2^31 / 2 and rounded up: tokens below 2^31 and 2^15 above them)
+    return __builtin_amdgcn_readfirstlane((int)(((uint32_t)(tokens < 1 ? 1 : tokens) + (uint32_t)per_step - 1) / (uint32_t)per_step)) * kPagedStep;
 }
 
 // The shares: the first `more` of them have one step more than the others.
@@ -257,11 +275,11 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
                 if (too_long && split == 0 && tid == 0) atomicOr(a.status, kStatusCapacityBit);
                 return;
             }
-            const int from = lo & ~31;
-            begin = from + split * a.chunk;
+            const int from = lo & ~31, chunk = paged_chunk(a);
+            begin = from + split * chunk;
             if (split > 0 && begin >= n) return;
-            end = n - begin < a.chunk ? n : begin + a.chunk;
-            whole = n - from <= a.chunk;
+            end = n - begin < chunk ? n : begin + chunk;
+            whole = n - from <= chunk;
             piece = ((int64_t)s * a.h_kv + kv) * a.ranges + split;
         }
 
@@ -521,8 +539,9 @@ __global__ void __launch_bounds__(256) swa_paged_join_chunks_kernel(PagedArgs a)
     const int s = blockIdx.x / a.h_q, hq = blockIdx.x - s * a.h_q, tid = threadIdx.x, team = tid / kLanes, lane = tid % kLanes;
     int row, lo, n;
     bool too_long;
-    if (!paged_sequence(a, s, row, lo, n, too_long) || n - (lo & ~31) <= a.chunk) return;
-    const int count = (n - (lo & ~31) + a.chunk - 1) / a.chunk, kv = hq / a.group, of = hq - kv * a.group;
+    const int chunk = paged_chunk(a);
+    if (!paged_sequence(a, s, row, lo, n, too_long) || n - (lo & ~31) <= chunk) return;
+    const int count = (n - (lo & ~31) + chunk - 1) / chunk, kv = hq / a.group, of = hq - kv * a.group;
     const int64_t stride = a.row_tiles * a.heads, first = ((int64_t)s * a.h_kv + kv) * a.ranges * stride + (of >> 4) * a.heads + (of & 15);
     __shared__ float weight[kPagedChunks], waves[4], waves2[4];
     __shared__ f32x4_t part[kTeams][kLanes];
@@ -662,8 +681,20 @@ int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_
     if (in_shares) {
         a.ranges = paged_max_shares(p);
     } else {
-        const int64_t of_one = steps / units, each = (of_one + paged_max_chunks(p) - 1) / paged_max_chunks(p);
-        a.chunk = (int32_t)(each * kPagedStep);
+        const int64_t of_one = steps / units;
+        // Work is even, so a call takes as long as the CU that has most of it.  us, as many chunks as make 1024 workgroups, 512, and by this rule (two
+        // on a CU before three before one): 131071 tokens, 4 key heads, 16 query heads each 54.5 / 50.4 / 50.4; 6 sequences of 32000, 8 key heads 126.8 /
+        // 155 (some CUs three) / 126.4; 2 of 10000, fp32 37.9 / 36.3 / 32.3.
+        int64_t least = INT64_MAX, each = of_one;        // steps of that CU, and of a workgroup
+        for (int k : {2, 3, 1}) {
+            const int64_t e = (of_one + paged_chunks(p, k) - 1) / paged_chunks(p, k), groups = paged_units(p) * ((of_one + e - 1) / e);
+            const int64_t most = (groups + 255) / 256 * e;
+            if (most < least) {
+                least = most;
+                each = e;
+            }
+        }
+        a.chunk = p.len_bound > 0 || p.b > 64 ? (int32_t)(each * kPagedStep) : 0;
         a.ranges = (int32_t)((of_one + each - 1) / each);
     }
     a.part_out = reinterpret_cast<float*>(static_cast<char*>(workspace) + kPagedPartialOffset);

@@ -283,11 +283,11 @@ def make_tables(lens, page, width, n_pages, seed):
 
 
 def check_decode(B, lens, h_q, h_kv, d, dtype, page, window=0, int8=False, scale=0.0, len_bound=0, row_start=None, n_rows=None, strided=False,
-                 spare=2, edit=None, bad=None, lse=True, loud=1.3, skipped=()):
+                 spare=2, edit=None, bad=None, lse=True, loud=1.3, skipped=(), wider=0):
     """loud: how large queries are (softmaxes that are nearly flat, or nearly one key's)."""
     b = len(lens)
     held = [-(-max(m, 0) // page) for m in lens]
-    n_pages, width = sum(held) + spare, max(max(held), 1)
+    n_pages, width = sum(held) + spare, max(max(held), 1) + wider
     table, free = make_tables(lens, page, width, n_pages, 11)
     k, v, ks, vs = make_pool(n_pages, h_kv, page, d, dtype, int8, 7)
     n_rows = n_rows or b
@@ -382,6 +382,14 @@ def test_long_caches_are_split_and_joined(B, dtype, int8):
     check_decode(B, [5000], 4, 1, 128, TYPES[dtype], 16, int8=int8, len_bound=5000)
     check_decode(B, [9000, 3, 0, 1025], 8, 2, 64, TYPES[dtype], 16, int8=int8)
     check_decode(B, [20011, 129], 3, 3, 64, TYPES[dtype], 64, int8=int8, window=7001)
+
+
+@pytest.mark.parametrize("len_bound", [0, 100000])
+def test_tables_far_wider_than_the_lengths(B, len_bound):
+    check_decode(B, [5000, 0, 700], 4, 1, 128, torch.bfloat16, 16, wider=7000, len_bound=len_bound)
+    check_decode(B, [3, 260], 4, 4, 64, torch.float16, 16, wider=130000, len_bound=len_bound)
+    check_decode(B, [3000, 260] * 16, 8, 2, 64, torch.float32, 16, wider=9000, len_bound=len_bound, window=900)
+    check_decode(B, [3000, 260] * 16, 8, 2, 64, torch.bfloat16, 16, wider=9000, len_bound=len_bound)
 
 
 def test_many_sequences(B):
