@@ -468,7 +468,7 @@ typedef struct {
     int32_t d;          /* head dimension, 64 or 128 */
     int32_t page_size;  /* tokens in a page, 1..SWA_MAX_CAP */
     int32_t n_pages;    /* pages in the pool; n_pages * h_kv * page_size < 2^31 */
-    int32_t max_pages;  /* width of the block table; max_pages * page_size < 2^31 */
+    int32_t max_pages;  /* width of the block table; max_pages * page_size <= 2^30 */
     int32_t dtype;      /* swa_dtype of q, k, v, weights, out, and of the pages without SWA_KV_INT8 */
     float scale;        /* logit scale; 0 selects 1/sqrt(d) */
     int32_t window;     /* 0, or how many of the last tokens the attention sees */

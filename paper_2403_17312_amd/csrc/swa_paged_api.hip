@@ -15,8 +15,8 @@ static int validate_paged(const swa_paged_params* p)
     if (p->b < 1 || p->b > SWA_MAX_PAGED_SEQS || p->h_q < 1 || p->h_q > 65535 || p->h_kv < 1 || p->h_q % p->h_kv != 0) return SWA_ERR_BAD_SHAPE;
     if (p->page_size < 1 || p->n_pages < 1 || p->max_pages < 1) return SWA_ERR_BAD_SHAPE;
     if (p->page_size > SWA_MAX_CAP) return SWA_ERR_CAPACITY;
-    // rows of the pool, and tokens of a sequence, are 32-bit numbers in the kernels (their bytes are not)
-    if ((int64_t)p->n_pages * p->page_size > 0x7fffffffLL / p->h_kv || (int64_t)p->max_pages * p->page_size > 0x7fffffffLL) return SWA_ERR_CAPACITY;
+    // rows of the pool, and tokens of a sequence with what a launch adds to them, are 32-bit numbers in the kernels (their bytes are not)
+    if ((int64_t)p->n_pages * p->page_size > 0x7fffffffLL / p->h_kv || (int64_t)p->max_pages * p->page_size > (1LL << 30)) return SWA_ERR_CAPACITY;
     if (!(p->scale >= 0.f) || isinf(p->scale) || !(p->eps >= 0.f) || isinf(p->eps)) return SWA_ERR_BAD_SHAPE;
     if (p->window < 0 || p->len_bound < 0) return SWA_ERR_BAD_SHAPE;
     if (p->flags & ~(SWA_KV_INT8 | SWA_ROPE_INTERLEAVED)) return SWA_ERR_BAD_SHAPE;

@@ -191,7 +191,7 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
     constexpr bool kCodes = std::is_same_v<C, Q8>, kWide = std::is_same_v<C, F32>;
     // Codes are exact in either 16-bit type.  Keys get the queries' type; values get bf16, whose range the weights need, which are products with a
     // scale there, and the weights go as two bf16 numbers, which hold 16 bits.
-    constexpr int kKeys = kWide ? 16 : 32, kTiles = kKeys / 16, kRow = D * Elem<C>::kBytes;
+    constexpr int kTiles = kWide && D == 128 ? 1 : 2, kKeys = 16 * kTiles, kRow = D * Elem<C>::kBytes;
     constexpr int kSteps = kWide ? D / 16 : D / 32;      // operands of a logit
     constexpr int kChannels = D / 16;                    // of V in a lane
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, j = lane >> 4;
@@ -209,6 +209,8 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
     bool too_long = false;
     Shares shares{0, 0};
     int4 begun = {0, 0, 0, 0};
+    const bool early = !SHARES && a.chunk && !a.window;
+    int early_page = 0;
     if constexpr (SHARES) {
         if (work >= a.ranges) return;
         __shared__ int wave_steps[kPagedWaves];
@@ -271,16 +273,17 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
             if (first == 0 && last < steps) begun = int4{1 + kv, row, shares.of(x + steps - 1) - work + 1, 0};
             x += last - first;
         } else {
-            if (!paged_sequence(a, s, row, lo, n, too_long)) {
-                if (too_long && split == 0 && tid == 0) atomicOr(a.status, kStatusCapacityBit);
-                return;
+            // Few sequences: a call is a chain of loads, so those whose place is known are under way before the length is (the page may be any
+            // of the sequence's row then, and counts for nothing where the tokens end earlier).
+            if (early) {
+                const int t = split * a.chunk + wave * kKeys + (lane & (kKeys - 1)), page = (int)(((uint64_t)(uint32_t)t * a.page_mul) >> a.page_shift);
+                early_page = a.block_table[(int64_t)s * a.max_pages + (page < a.max_pages ? page : a.max_pages - 1)];
             }
-            const int from = lo & ~31, chunk = paged_chunk(a);
-            begin = from + split * chunk;
-            if (split > 0 && begin >= n) return;
-            end = n - begin < chunk ? n : begin + chunk;
-            whole = n - from <= chunk;
-            piece = ((int64_t)s * a.h_kv + kv) * a.ranges + split;
+            row = s;
+            if (a.row_start) {
+                row = a.row_start[s + 1] - 1;
+                if (row < a.row_start[s] || row >= a.n_rows) return;
+            }
         }
 
         // Query operands: column col is query head 16 tile + col of the group.
@@ -296,6 +299,19 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
             }
         }
 
+        if constexpr (!SHARES) {
+            if (!paged_sequence(a, s, row, lo, n, too_long)) {
+                if (too_long && split == 0 && tid == 0) atomicOr(a.status, kStatusCapacityBit);
+                return;
+            }
+            const int from = lo & ~31, chunk = paged_chunk(a);
+            begin = from + split * chunk;
+            if (split > 0 && begin >= n) return;
+            end = n - begin < chunk ? n : begin + chunk;
+            whole = n - from <= chunk;
+            piece = ((int64_t)s * a.h_kv + kv) * a.ranges + split;
+        }
+
         float top = -INFINITY, sum = 0.f;                    // of column col, the sum of this lane's keys alone
         f32x4_t acc[kChannels];
 #pragma unroll
@@ -303,14 +319,13 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
         const int32_t* const table = a.block_table + (int64_t)s * a.max_pages;
         bool bad = false;
 
-        // Row of the pool that holds this lane's token of the tile at `base` (-1: none).
-        auto token_page = [&](int base, int& off) {
-            const int t = base + (lane & (kKeys - 1));
-            const int clamped = t < lo ? lo : (t < n ? t : n - 1);
-            const int page = (int)(((uint64_t)(uint32_t)clamped * a.page_mul) >> a.page_shift);
-            off = clamped - page * a.page_size;
-            return table[page];
+        // Page that holds this lane's token of the tile at `base`, and the token's place there.
+        auto page_of = [&](int base) {
+            const int t = base + (lane & (kKeys - 1)), there = t < lo ? lo : (t < n ? t : n - 1);
+            return (int)(((uint64_t)(uint32_t)there * a.page_mul) >> a.page_shift);
         };
+        auto token_page = [&](int base) { return table[page_of(base)]; };
+        auto token_off = [&](int base) { return base + (lane & (kKeys - 1)) - page_of(base) * a.page_size; };
         constexpr int kLoads = kCodes ? D / 64 : kSteps, kVLoad = kWide ? D / 64 : 1, kVBytes = kWide ? 16 : kChannels * Elem<C>::kBytes;
         struct alignas(kVBytes < 16 ? kVBytes : 16) Values { uint32_t w[kVBytes / 4]; };
 
@@ -419,31 +434,42 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
 
             if constexpr (kWide) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+                for (int u = 0; u < kTiles; ++u)
 #pragma unroll
-                    for (int e = 0; e < kChannels; ++e)
-                        acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(u2f(v[0][i][e / 4].w[e % 4]), x[0][i], acc[e], 0, 0, 0);
-            } else if constexpr (kCodes) {
-                const Vec16 p = {round2<BF16>(x[0][0], x[0][1]), round2<BF16>(x[0][2], x[0][3]), round2<BF16>(x[1][0], x[1][1]), round2<BF16>(x[1][2], x[1][3])};
-                float f[8];
-                unpack<BF16>(p, f);
-                const Vec16 p_rest = {round2<BF16>(x[0][0] - f[0], x[0][1] - f[1]), round2<BF16>(x[0][2] - f[2], x[0][3] - f[3]),
-                                      round2<BF16>(x[1][0] - f[4], x[1][1] - f[5]), round2<BF16>(x[1][2] - f[6], x[1][3] - f[7])};
+                    for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int e = 0; e < kChannels; ++e) {
-                    auto c = [&](int u, int i) { return code(v[u][i][0].w[e / 4], e % 4); };
-                    const Vec16 op = {round2<BF16>(c(0, 0), c(0, 1)), round2<BF16>(c(0, 2), c(0, 3)), round2<BF16>(c(1, 0), c(1, 1)),
-                                      round2<BF16>(c(1, 2), c(1, 3))};
-                    acc[e] = mfma16<BF16>(op, p, acc[e]);
-                    acc[e] = mfma16<BF16>(op, p_rest, acc[e]);
-                }
+                        for (int e = 0; e < kChannels; ++e)
+                            acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(u2f(v[u][i][e / 4].w[e % 4]), x[u][i], acc[e], 0, 0, 0);
             } else {
-                const Vec16 p = {round2<T>(x[0][0], x[0][1]), round2<T>(x[0][2], x[0][3]), round2<T>(x[1][0], x[1][1]), round2<T>(x[1][2], x[1][3])};
 #pragma unroll
-                for (int e = 0; e < kChannels; ++e) {
-                    constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;
-                    auto two = [&](int u, int i) { return __builtin_amdgcn_perm(v[u][i + 1][0].w[e / 2], v[u][i][0].w[e / 2], e & 1 ? kHigh : kLow); };
-                    acc[e] = mfma16<T>(Vec16{two(0, 0), two(0, 2), two(1, 0), two(1, 2)}, p, acc[e]);
+                for (int u = 0; u < kTiles; u += 2) {        // 32 keys a product
+                    constexpr bool kRest = kCodes;
+                    typedef std::conditional_t<kCodes, BF16, T> P;
+                    const Vec16 p = {round2<P>(x[u][0], x[u][1]), round2<P>(x[u][2], x[u][3]), round2<P>(x[u + 1][0], x[u + 1][1]),
+                                     round2<P>(x[u + 1][2], x[u + 1][3])};
+                    Vec16 p_rest{};
+                    if constexpr (kRest) {
+                        float f[8];
+                        unpack<BF16>(p, f);
+                        p_rest = {round2<BF16>(x[u][0] - f[0], x[u][1] - f[1]), round2<BF16>(x[u][2] - f[2], x[u][3] - f[3]),
+                                  round2<BF16>(x[u + 1][0] - f[4], x[u + 1][1] - f[5]), round2<BF16>(x[u + 1][2] - f[6], x[u + 1][3] - f[7])};
+                    }
+#pragma unroll
+                    for (int e = 0; e < kChannels; ++e) {
+                        if constexpr (kCodes) {
+                            auto c = [&](int w, int i) { return code(v[u + w][i][0].w[e / 4], e % 4); };
+                            const Vec16 op = {round2<BF16>(c(0, 0), c(0, 1)), round2<BF16>(c(0, 2), c(0, 3)), round2<BF16>(c(1, 0), c(1, 1)),
+                                              round2<BF16>(c(1, 2), c(1, 3))};
+                            acc[e] = mfma16<BF16>(op, p, acc[e]);
+                            acc[e] = mfma16<BF16>(op, p_rest, acc[e]);
+                        } else {
+                            constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;
+                            auto two = [&](int w, int i) {
+                                return __builtin_amdgcn_perm(v[u + w][i + 1][0].w[e / 2], v[u + w][i][0].w[e / 2], e & 1 ? kHigh : kLow);
+                            };
+                            acc[e] = mfma16<T>(Vec16{two(0, 0), two(0, 2), two(1, 0), two(1, 2)}, p, acc[e]);
+                        }
+                    }
                 }
             }
         };
@@ -451,34 +477,44 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
         // Whole tiles first; the others, at the ends of the window and where a page is not in the pool, in a loop of their own, whose addresses then
         // take no registers from this one.
         constexpr int kStride = kPagedWaves * kKeys;
-        const int tile0 = begin + wave * kKeys;
-        auto row_of = [&](int base, int page, int off) {
+        // The pool's rows of a tile's tokens, -1 where there is none.
+        auto row_of = [&](int base, int page) {
             const int t = base + (lane & (kKeys - 1));
-            return (uint32_t)page < (uint32_t)a.n_pages && t >= lo && t < n ? (page * a.h_kv + kv) * a.page_size + off : -1;
+            const bool live = t >= lo && t < n, in_pool = (uint32_t)page < (uint32_t)a.n_pages;
+            bad |= live && !in_pool;
+            return live && in_pool ? (page * a.h_kv + kv) * a.page_size + token_off(base) : -1;
         };
-        int left0 = tile0, left1 = end;                      // tiles that are left
+        int next = begin + wave * kKeys, page = 0;
+        if (next < end) page = early ? early_page : token_page(next);
+        int left = next, left_end = end, r = 0;              // tiles that are left: from, up to, and the first one's rows
         if (a.sixteens) {
-            left0 = end;
-            left1 = begin;
-            int next_off = 0, next_page = tile0 < end ? token_page(tile0, next_off) : 0;
-            for (int base = tile0; base < end; base += kStride) {
-                const int page = next_page, off = next_off;
-                if (base + kStride < end) next_page = token_page(base + kStride, next_off);
-                const int r = row_of(base, page, off);
-                if (!__any(r < 0)) {
-                    take(std::true_type{}, r);
+            left = end;
+            left_end = begin;
+            while (next < end) {
+                const int base = next, this_page = page;
+                next += kStride;
+                if (next < end) page = token_page(next);
+                const int rows = row_of(base, this_page);
+                if (!__any(rows < 0)) {
+                    take(std::true_type{}, rows);
                 } else {
-                    left0 = base < left0 ? base : left0;
-                    left1 = base + 1;
+                    if (left == end) {
+                        left = base;
+                        r = rows;
+                    }
+                    left_end = base + 1;
                 }
             }
+        } else if (next < end) {
+            r = row_of(next, page);
         }
-        for (int base = left0; base < left1; base += kStride) {
-            int off = 0;
-            const int page = token_page(base, off), r = row_of(base, page, off), t = base + (lane & (kKeys - 1));
-            if (a.sixteens && !__any(r < 0)) continue;
-            bad |= (uint32_t)page >= (uint32_t)a.n_pages && t >= lo && t < n;
+        while (left < left_end) {
             take(std::false_type{}, r);
+            do {
+                left += kStride;
+                if (left >= left_end) break;
+                r = row_of(left, token_page(left));
+            } while (a.sixteens && !__any(r < 0));
         }
         if (bad) atomicOr(a.status, kStatusBadRequestBit);
 
@@ -537,15 +573,20 @@ __global__ void __launch_bounds__(256) swa_paged_join_chunks_kernel(PagedArgs a)
 {
     constexpr int kLanes = D / 4, kTeams = 256 / kLanes;
     const int s = blockIdx.x / a.h_q, hq = blockIdx.x - s * a.h_q, tid = threadIdx.x, team = tid / kLanes, lane = tid % kLanes;
+    const int kv = hq / a.group, of = hq - kv * a.group;
+    const int64_t stride = a.row_tiles * a.heads, first = ((int64_t)s * a.h_kv + kv) * a.ranges * stride + (of >> 4) * a.heads + (of & 15);
+    __shared__ float weight[kPagedChunks], waves[4], waves2[4];
+    __shared__ f32x4_t part[kTeams][kLanes];
+    // (what may turn out not to be a chunk's is loaded all the same, while the length is on its way)
+    float2 mine = tid < a.ranges ? *reinterpret_cast<const float2*>(a.part_sum + (first + tid * stride) * 2) : float2{-INFINITY, 0.f};
+    f32x4_t y = {0.f, 0.f, 0.f, 0.f};
+    if (team < a.ranges) y = *reinterpret_cast<const f32x4_t*>(a.part_out + (first + team * stride) * D + lane * 4);
     int row, lo, n;
     bool too_long;
     const int chunk = paged_chunk(a);
     if (!paged_sequence(a, s, row, lo, n, too_long) || n - (lo & ~31) <= chunk) return;
-    const int count = (n - (lo & ~31) + chunk - 1) / chunk, kv = hq / a.group, of = hq - kv * a.group;
-    const int64_t stride = a.row_tiles * a.heads, first = ((int64_t)s * a.h_kv + kv) * a.ranges * stride + (of >> 4) * a.heads + (of & 15);
-    __shared__ float weight[kPagedChunks], waves[4], waves2[4];
-    __shared__ f32x4_t part[kTeams][kLanes];
-    const float2 mine = tid < count ? *reinterpret_cast<const float2*>(a.part_sum + (first + tid * stride) * 2) : float2{-INFINITY, 0.f};
+    const int count = (n - (lo & ~31) + chunk - 1) / chunk;
+    mine = tid < count ? mine : float2{-INFINITY, 0.f};
     float top = wave_max(mine.x);
     if ((tid & 63) == 0) waves[tid >> 6] = top;
     __syncthreads();
@@ -556,9 +597,9 @@ __global__ void __launch_bounds__(256) swa_paged_join_chunks_kernel(PagedArgs a)
     if ((tid & 63) == 0) waves2[tid >> 6] = sum;
     __syncthreads();
     const float total = (waves2[0] + waves2[1]) + (waves2[2] + waves2[3]);
-    f32x4_t y = {0.f, 0.f, 0.f, 0.f};
+    y = team < count ? y * weight[team] : f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-    for (int i = team; i < count; i += kTeams) y += *reinterpret_cast<const f32x4_t*>(a.part_out + (first + i * stride) * D + lane * 4) * weight[i];
+    for (int i = team + kTeams; i < count; i += kTeams) y += *reinterpret_cast<const f32x4_t*>(a.part_out + (first + i * stride) * D + lane * 4) * weight[i];
     part[team][lane] = y;
     __syncthreads();
     if (team) return;

@@ -78,7 +78,7 @@ def test_params_struct_matches_header(B):
     (dict(max_pages=0), "SWA_ERR_BAD_SHAPE"),
     (dict(page_size=16385), "SWA_ERR_CAPACITY"),
     (dict(n_pages=1 << 26), "SWA_ERR_CAPACITY"),     # 2^26 pages of 16 tokens and 2 heads: 2^31 rows
-    (dict(max_pages=1 << 27), "SWA_ERR_CAPACITY"),
+    (dict(max_pages=(1 << 26) + 1), "SWA_ERR_CAPACITY"),
     (dict(scale=-1.0), "SWA_ERR_BAD_SHAPE"),
     (dict(scale=float("inf")), "SWA_ERR_BAD_SHAPE"),
     (dict(eps=float("nan")), "SWA_ERR_BAD_SHAPE"),
