@@ -41,7 +41,7 @@ static int check_rows(const swa_paged_params& p, const swa_rows& r, int heads)
 static int check_pool(const swa_paged_params& p, const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale)
 {
     if (!k_pages || !v_pages || (paged_int8(p) && (!k_scale || !v_scale))) return SWA_ERR_NULL;
-    return on16(k_pages) && on16(v_pages) ? SWA_OK : SWA_ERR_ALIGNMENT;
+    return on16(k_pages) && on16(v_pages) && (!paged_int8(p) || (on16(k_scale) && on16(v_scale))) ? SWA_OK : SWA_ERR_ALIGNMENT;
 }
 
 __global__ void swa_paged_zero_kernel(int32_t* p)
@@ -96,7 +96,7 @@ int swa_paged_plan(const swa_paged_params* params, const int32_t* new_cnt, const
         return SWA_ERR_NULL;
     if (max_rows < 1 || max_rows > swa::kMaxPlanRows) return SWA_ERR_BAD_SHAPE;
     // (workgroups read the old lists while others write the new ones)
-    if (cache_len == new_len || free_state == free_state_out) return SWA_ERR_BAD_SHAPE;
+    if (cache_len == new_len || new_cnt == new_len || free_state == free_state_out) return SWA_ERR_BAD_SHAPE;
     return swa::launch_paged_plan(*params, new_cnt, cache_len, new_len, block_table, free_ring, free_state, free_state_out, max_rows,
                                   row_start, slot, pos, workspace, static_cast<hipStream_t>(stream));
 }

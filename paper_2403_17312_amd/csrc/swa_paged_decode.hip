@@ -1,7 +1,7 @@
 // Attention of one new token per sequence over a paged cache.  Bound by HBM: every key and value of the window is read once, 4 flops for
 // two elements and query head.
 //
-// A workgroup serves up to 16 of the query heads that share a key head, over a range of one sequence's tokens; its four waves take tiles of the range
+// A workgroup serves up to 16 (or 32) of the query heads that share a key head, over a range of one sequence's tokens; its four waves take tiles of the range
 // in turn, each with a running maximum and sum of the softmax.  Ranges come in two ways:
 //   chunks   few sequences: each one's tokens in equal chunks, as many as fill the CUs evenly, a workgroup for each.
 //   shares   many, and long ones: the call's work, in steps of 128 tokens of one sequence and key head, laid end to end and cut into as
@@ -36,7 +36,7 @@ struct PagedArgs {
     int4* begun;                                   // [shares]: key head, row, pieces of the sequence that a share begins and does not end (x = 0: none)
     int32_t* status;
     int32_t b, n_rows, h_q, h_kv, page_size, n_pages, max_pages, window, len_max;
-    int32_t group, row_tiles, heads;               // query heads of a key head, tiles of 16 of them, heads of a tile at most
+    int32_t group, row_tiles, heads, tile_heads;   // query heads of a key head, tiles of them, heads of a tile that there are at most, and that fit
     int32_t ranges;                                // shares, or chunks of a sequence at most
     int32_t chunk;                                 // tokens; 0: the longest sequence says
     uint32_t page_mul;                             // t / page_size = t * page_mul >> page_shift for 0 <= t < 2^31
@@ -49,7 +49,10 @@ constexpr int kPagedWaves = 4;
 constexpr int kPagedStep = 128;                    // tokens
 constexpr int kPagedChunks = 256;                  // chunks of a sequence at most, which bounds what the join of one has to read
 
-static int row_tiles_of(const swa_paged_params& p) { return (p.h_q / p.h_kv + 15) / 16; }
+// Query heads of a workgroup: the matrix cores' 16 columns, or twice as many, so that keys and values shared by more heads are read half as often.
+static int tile_heads_of(const swa_paged_params& p) { return p.h_q / p.h_kv > 16 ? 32 : 16; }
+
+static int row_tiles_of(const swa_paged_params& p) { return (p.h_q / p.h_kv + tile_heads_of(p) - 1) / tile_heads_of(p); }
 
 // Tokens of a sequence that a call may see, from a multiple of 32 on.
 static int64_t paged_span(const swa_paged_params& p)
@@ -69,14 +72,15 @@ static bool paged_in_shares(const swa_paged_params& p)
 
 static int64_t paged_units(const swa_paged_params& p) { return (int64_t)p.b * p.h_kv * row_tiles_of(p); }
 
-constexpr bool paged_two(int row_bytes) { return row_bytes == 512; }
+constexpr bool paged_two(int row_bytes, int rows, int d) { return row_bytes == 512 || (rows == 2 && d == 128); }
 
-// Shares of a call at most: the workgroups that the chip holds at once.  A CU has four of 64 channels, three of 128 (168 registers a lane), two of 128
-// in fp32, which do not fit those (64 sequences of 4352 tokens, 8 key heads: three with spills 381 us, two 356).  768 / 1024 shares of 128
+// Shares of a call at most: the workgroups that the chip holds at once.  A CU has four of 64 channels in 16 bits, three of 64 in fp32 and of 128 (168
+// registers a lane), two of 128 in fp32 and of 128 with 32 heads, which do not fit those (64 sequences of 4352 tokens, 8 key heads: three with spills 381 us, two 356).  768 / 1024 shares of 128
 // channels: the ragged 128 sequences below 345 / 387 us; 64 of 100..8001 tokens in 8 bits 107 / 123.
 static int paged_max_shares(const swa_paged_params& p)
 {
-    const int n = (p.d == 64 ? 1024 : paged_two(paged_row_bytes(p)) ? 512 : 768) / row_tiles_of(p);
+    const bool two = paged_two(paged_row_bytes(p), tile_heads_of(p) / 16, p.d);
+    const int n = (two ? 512 : p.d == 64 && tile_heads_of(p) == 16 && p.dtype != SWA_F32 ? 1024 : 768) / row_tiles_of(p);
     return n < 1 ? 1 : n;
 }
 
@@ -94,7 +98,7 @@ static int64_t paged_piece_rows(const swa_paged_params& p)
     const int64_t shares = 2 * (int64_t)paged_max_shares(p) * row_tiles_of(p);
     const int64_t chunks = paged_chunks(p, 3) > 1 ? paged_chunks(p, 3) * paged_units(p) : 0;
     const int64_t pieces = paged_units(p) >= 64 && shares > chunks ? shares : chunks;
-    return 2 * ((pieces * (group < 16 ? group : 16) + 1) / 2);
+    return 2 * ((pieces * (group < tile_heads_of(p) ? group : tile_heads_of(p)) + 1) / 2);
 }
 
 size_t paged_partial_bytes(const swa_paged_params& p)
@@ -185,20 +189,20 @@ struct Shares {
 };
 
 // T: type of queries and outputs, C: of the pages (Q8: codes).
-template <typename T, typename C, int D, bool SHARES>
-__global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * D) ? 2 : 3) swa_paged_decode_kernel(PagedArgs a)
+template <typename T, typename C, int D, bool SHARES, int ROWS>
+__global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * D, ROWS, D) ? 2 : 3) swa_paged_decode_kernel(PagedArgs a)
 {
     constexpr bool kCodes = std::is_same_v<C, Q8>, kWide = std::is_same_v<C, F32>;
     // Codes are exact in either 16-bit type.  Keys get the queries' type; values get bf16, whose range the weights need, which are products with a
     // scale there, and the weights go as two bf16 numbers, which hold 16 bits.
-    constexpr int kTiles = kWide && D == 128 ? 1 : 2, kKeys = 16 * kTiles, kRow = D * Elem<C>::kBytes;
+    constexpr int kTiles = kWide && (D == 128 || ROWS == 2) ? 1 : 2, kKeys = 16 * kTiles, kRow = D * Elem<C>::kBytes;
     constexpr int kSteps = kWide ? D / 16 : D / 32;      // operands of a logit
     constexpr int kChannels = D / 16;                    // of V in a lane
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, j = lane >> 4;
 
     // Row tiles of one range read the same pages: eight ranges, then the same ones' next row tile, so that they meet in one XCD's L2.
     const int eighth = blockIdx.x >> 3, work = (eighth / a.row_tiles) * 8 + (blockIdx.x & 7), tile = eighth % a.row_tiles;
-    const int heads = a.group - 16 * tile < 16 ? a.group - 16 * tile : 16;
+    const int heads = a.group - 16 * ROWS * tile < 16 * ROWS ? a.group - 16 * ROWS * tile : 16 * ROWS;
 
     constexpr int kPitch = D + 4;
     __shared__ float part[kPagedWaves][16][kPitch];
@@ -286,17 +290,19 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
             }
         }
 
-        // Query operands: column col is query head 16 tile + col of the group.
-        const int64_t head0 = (int64_t)kv * a.group + 16 * tile;
-        Vec16 q[kSteps];
+        // Query operands: column col is query head 16 (ROWS tile + g) + col of the group.
+        const int64_t head0 = (int64_t)kv * a.group + 16 * ROWS * tile;
+        Vec16 q[ROWS][kSteps];
         {
             const char* const from = a.q + row * a.q_stride + (head0 + col) * (D * Elem<T>::kBytes);
 #pragma unroll
-            for (int c = 0; c < kSteps; ++c) {
-                // (16 bytes of codes are two operands' channels)
-                const int at = kCodes ? (c / 2) * 64 + j * 16 + (c & 1) * 8 : kWide ? c * 16 + j * 4 : c * 32 + j * 8;
-                q[c] = col < heads ? load16(from + at * Elem<T>::kBytes) : Vec16{0u, 0u, 0u, 0u};
-            }
+            for (int g = 0; g < ROWS; ++g)
+#pragma unroll
+                for (int c = 0; c < kSteps; ++c) {
+                    // (16 bytes of codes are two operands' channels)
+                    const int at = kCodes ? (c / 2) * 64 + j * 16 + (c & 1) * 8 : kWide ? c * 16 + j * 4 : c * 32 + j * 8;
+                    q[g][c] = 16 * g + col < heads ? load16(from + (16 * g * D + at) * Elem<T>::kBytes) : Vec16{0u, 0u, 0u, 0u};
+                }
         }
 
         if constexpr (!SHARES) {
@@ -312,10 +318,15 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
             piece = ((int64_t)s * a.h_kv + kv) * a.ranges + split;
         }
 
-        float top = -INFINITY, sum = 0.f;                    // of column col, the sum of this lane's keys alone
-        f32x4_t acc[kChannels];
+        float top[ROWS], sum[ROWS];                          // of column col, the sum of this lane's keys alone
+        f32x4_t acc[ROWS][kChannels];
 #pragma unroll
-        for (int e = 0; e < kChannels; ++e) acc[e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        for (int g = 0; g < ROWS; ++g) {
+            top[g] = -INFINITY;
+            sum[g] = 0.f;
+#pragma unroll
+            for (int e = 0; e < kChannels; ++e) acc[g][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        }
         const int32_t* const table = a.block_table + (int64_t)s * a.max_pages;
         bool bad = false;
 
@@ -380,57 +391,71 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
             }
 
             __builtin_amdgcn_sched_barrier(0);
-            float x[kTiles][4];
+            float x[ROWS][kTiles][4];
 #pragma unroll
             for (int u = 0; u < kTiles; ++u) {
-                f32x4_t logit = {0.f, 0.f, 0.f, 0.f};
+                f32x4_t logit[ROWS];
+#pragma unroll
+                for (int g = 0; g < ROWS; ++g) logit[g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int c = 0; c < kSteps; ++c) {
+                    Vec16 op;
                     if constexpr (kCodes) {
                         const Vec16& b = k[u][c / 2];
                         const uint32_t w[2] = {c & 1 ? b.z : b.x, c & 1 ? b.w : b.y};
-                        const Vec16 op = {round2<T>(code(w[0], 0), code(w[0], 1)), round2<T>(code(w[0], 2), code(w[0], 3)),
-                                          round2<T>(code(w[1], 0), code(w[1], 1)), round2<T>(code(w[1], 2), code(w[1], 3))};
-                        logit = mfma16<T>(op, q[c], logit);
+                        op = Vec16{round2<T>(code(w[0], 0), code(w[0], 1)), round2<T>(code(w[0], 2), code(w[0], 3)),
+                                   round2<T>(code(w[1], 0), code(w[1], 1)), round2<T>(code(w[1], 2), code(w[1], 3))};
                     } else {
-                        logit = mfma16<T>(k[u][c], q[c], logit);
+                        op = k[u][c];
                     }
+#pragma unroll
+                    for (int g = 0; g < ROWS; ++g) logit[g] = mfma16<T>(op, q[g][c], logit[g]);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[u][i] = logit[i] * a.scale;
-                    if constexpr (kCodes) x[u][i] *= k_scale[u][i];
-                    if constexpr (!kWhole) x[u][i] = rv[u][i] < 0 ? -INFINITY : x[u][i];
-                }
+                for (int g = 0; g < ROWS; ++g)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        x[g][u][i] = logit[g][i] * a.scale;
+                        if constexpr (kCodes) x[g][u][i] *= k_scale[u][i];
+                        if constexpr (!kWhole) x[g][u][i] = rv[u][i] < 0 ? -INFINITY : x[g][u][i];
+                    }
             }
-            float most = x[0][0];
+            if constexpr (!kWhole) {                         // (a weight of 0 times what is no number is none either)
 #pragma unroll
-            for (int i = 1; i < 4 * kTiles; ++i) most = fmaxf(most, x[i / 4][i % 4]);
-            most = fmaxf(most, __shfl_xor(most, 16, 64));
-            most = fmaxf(most, __shfl_xor(most, 32, 64));
-            if (__any(most > top)) {
-                const float to = fmaxf(top, most), down = __builtin_amdgcn_exp2f(top - (to == -INFINITY ? 0.f : to));
-                top = to;
-                sum *= down;
+                for (int u = 0; u < kTiles; ++u)
 #pragma unroll
-                for (int e = 0; e < kChannels; ++e) acc[e] *= down;
-            }
-            const float from = top == -INFINITY ? 0.f : top;
-#pragma unroll
-            for (int u = 0; u < kTiles; ++u)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[u][i] = __builtin_amdgcn_exp2f(x[u][i] - from);
-                    sum += x[u][i];
-                    if constexpr (kCodes) x[u][i] *= v_scale[u][i];
-                    if constexpr (!kWhole) {                 // (a weight of 0 times what is no number is none either)
+                    for (int i = 0; i < 4; ++i) {
                         const uint32_t keep = rv[u][i] < 0 ? 0u : ~0u;
 #pragma unroll
                         for (int y = 0; y < kVLoad; ++y)
 #pragma unroll
                             for (int z = 0; z < kVBytes / 4; ++z) v[u][i][y].w[z] &= keep;
                     }
+            }
+#pragma unroll
+            for (int g = 0; g < ROWS; ++g) {
+                float most = x[g][0][0];
+#pragma unroll
+                for (int i = 1; i < 4 * kTiles; ++i) most = fmaxf(most, x[g][i / 4][i % 4]);
+                most = fmaxf(most, __shfl_xor(most, 16, 64));
+                most = fmaxf(most, __shfl_xor(most, 32, 64));
+                if (__any(most > top[g])) {
+                    const float to = fmaxf(top[g], most), down = __builtin_amdgcn_exp2f(top[g] - (to == -INFINITY ? 0.f : to));
+                    top[g] = to;
+                    sum[g] *= down;
+#pragma unroll
+                    for (int e = 0; e < kChannels; ++e) acc[g][e] *= down;
                 }
+                const float from = top[g] == -INFINITY ? 0.f : top[g];
+#pragma unroll
+                for (int u = 0; u < kTiles; ++u)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        x[g][u][i] = __builtin_amdgcn_exp2f(x[g][u][i] - from);
+                        sum[g] += x[g][u][i];
+                        if constexpr (kCodes) x[g][u][i] *= v_scale[u][i];
+                    }
+            }
 
             if constexpr (kWide) {
 #pragma unroll
@@ -439,35 +464,43 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
                         for (int e = 0; e < kChannels; ++e)
-                            acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(u2f(v[u][i][e / 4].w[e % 4]), x[u][i], acc[e], 0, 0, 0);
+#pragma unroll
+                            for (int g = 0; g < ROWS; ++g)
+                                acc[g][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(u2f(v[u][i][e / 4].w[e % 4]), x[g][u][i], acc[g][e], 0, 0, 0);
             } else {
 #pragma unroll
                 for (int u = 0; u < kTiles; u += 2) {        // 32 keys a product
-                    constexpr bool kRest = kCodes;
                     typedef std::conditional_t<kCodes, BF16, T> P;
-                    const Vec16 p = {round2<P>(x[u][0], x[u][1]), round2<P>(x[u][2], x[u][3]), round2<P>(x[u + 1][0], x[u + 1][1]),
-                                     round2<P>(x[u + 1][2], x[u + 1][3])};
-                    Vec16 p_rest{};
-                    if constexpr (kRest) {
-                        float f[8];
-                        unpack<BF16>(p, f);
-                        p_rest = {round2<BF16>(x[u][0] - f[0], x[u][1] - f[1]), round2<BF16>(x[u][2] - f[2], x[u][3] - f[3]),
-                                  round2<BF16>(x[u + 1][0] - f[4], x[u + 1][1] - f[5]), round2<BF16>(x[u + 1][2] - f[6], x[u + 1][3] - f[7])};
+                    Vec16 p[ROWS], p_rest[ROWS];
+#pragma unroll
+                    for (int g = 0; g < ROWS; ++g) {
+                        const float* const w = x[g][u];
+                        p[g] = Vec16{round2<P>(w[0], w[1]), round2<P>(w[2], w[3]), round2<P>(w[4], w[5]), round2<P>(w[6], w[7])};
+                        if constexpr (kCodes) {
+                            float f[8];
+                            unpack<BF16>(p[g], f);
+                            p_rest[g] = Vec16{round2<BF16>(w[0] - f[0], w[1] - f[1]), round2<BF16>(w[2] - f[2], w[3] - f[3]),
+                                              round2<BF16>(w[4] - f[4], w[5] - f[5]), round2<BF16>(w[6] - f[6], w[7] - f[7])};
+                        }
                     }
 #pragma unroll
                     for (int e = 0; e < kChannels; ++e) {
+                        Vec16 op;
                         if constexpr (kCodes) {
                             auto c = [&](int w, int i) { return code(v[u + w][i][0].w[e / 4], e % 4); };
-                            const Vec16 op = {round2<BF16>(c(0, 0), c(0, 1)), round2<BF16>(c(0, 2), c(0, 3)), round2<BF16>(c(1, 0), c(1, 1)),
-                                              round2<BF16>(c(1, 2), c(1, 3))};
-                            acc[e] = mfma16<BF16>(op, p, acc[e]);
-                            acc[e] = mfma16<BF16>(op, p_rest, acc[e]);
+                            op = Vec16{round2<BF16>(c(0, 0), c(0, 1)), round2<BF16>(c(0, 2), c(0, 3)), round2<BF16>(c(1, 0), c(1, 1)),
+                                       round2<BF16>(c(1, 2), c(1, 3))};
                         } else {
                             constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;
                             auto two = [&](int w, int i) {
                                 return __builtin_amdgcn_perm(v[u + w][i + 1][0].w[e / 2], v[u + w][i][0].w[e / 2], e & 1 ? kHigh : kLow);
                             };
-                            acc[e] = mfma16<T>(Vec16{two(0, 0), two(0, 2), two(1, 0), two(1, 2)}, p, acc[e]);
+                            op = Vec16{two(0, 0), two(0, 2), two(1, 0), two(1, 2)};
+                        }
+#pragma unroll
+                        for (int g = 0; g < ROWS; ++g) {
+                            acc[g][e] = mfma16<P>(op, p[g], acc[g][e]);
+                            if constexpr (kCodes) acc[g][e] = mfma16<BF16>(op, p_rest[g], acc[g][e]);
                         }
                     }
                 }
@@ -522,44 +555,47 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
         int who = tid;
         if (SHARES) asm volatile("" : "+v"(who));            // (addresses made from it are not kept in registers around the loop)
         const int to_col = who & 15, to_j = (who >> 4) & 3;
-        sum += __shfl_xor(sum, 16, 64);
-        sum += __shfl_xor(sum, 32, 64);
-        __syncthreads();                                     // (the piece before this one has been read)
-        if (to_j == 0) {
-            tops[wave][to_col] = top;
-            sums[wave][to_col] = sum;
-        }
 #pragma unroll
-        for (int e = 0; e < kChannels; ++e)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) part[wave][to_col][kWide ? (e / 4) * 64 + (4 * to_j + i) * 4 + e % 4 : (4 * to_j + i) * kChannels + e] = acc[e][i];
-        __syncthreads();
-        const int head = who >> 4;
-        if (head < heads) {
-            float all = tops[0][head];
-#pragma unroll
-            for (int w = 1; w < kPagedWaves; ++w) all = fmaxf(all, tops[w][head]);
-            float total = 0.f, y[kChannels] = {};
-#pragma unroll
-            for (int w = 0; w < kPagedWaves; ++w) {
-                const float f = __builtin_amdgcn_exp2f(tops[w][head] - (all == -INFINITY ? 0.f : all));
-                total = __builtin_fmaf(sums[w][head], f, total);
-#pragma unroll
-                for (int e = 0; e < kChannels; ++e) y[e] = __builtin_fmaf(part[w][head][(who & 15) * kChannels + e], f, y[e]);
+        for (int g = 0; g < ROWS; ++g) {
+            sum[g] += __shfl_xor(sum[g], 16, 64);
+            sum[g] += __shfl_xor(sum[g], 32, 64);
+            __syncthreads();                                     // (what was there before has been read)
+            if (to_j == 0) {
+                tops[wave][to_col] = top[g];
+                sums[wave][to_col] = sum[g];
             }
-            if (whole) {
-                const int64_t at = (int64_t)row * a.h_q + head0 + head;
-                const float inverse = 1.f / total;
-                char* const to = a.out + at * (D * Elem<T>::kBytes);
 #pragma unroll
-                for (int e = 0; e < kChannels; ++e) store_elem<T>(to, (who & 15) * kChannels + e, total == 0.f ? 0.f : y[e] * inverse);
-                if (a.lse && (who & 15) == 0) a.lse[at] = (all + __builtin_log2f(total)) * 0.69314718055994530942f;
-            } else {
-                const int64_t at = (piece * a.row_tiles + tile) * a.heads + head;
+            for (int e = 0; e < kChannels; ++e)
 #pragma unroll
-                for (int e = 0; e < kChannels; e += 4)
-                    *reinterpret_cast<f32x4_t*>(a.part_out + at * D + (who & 15) * kChannels + e) = f32x4_t{y[e], y[e + 1], y[e + 2], y[e + 3]};
-                if ((who & 15) == 0) *reinterpret_cast<float2*>(a.part_sum + at * 2) = float2{all, total};
+                for (int i = 0; i < 4; ++i) part[wave][to_col][kWide ? (e / 4) * 64 + (4 * to_j + i) * 4 + e % 4 : (4 * to_j + i) * kChannels + e] = acc[g][e][i];
+            __syncthreads();
+            const int head = who >> 4;
+            if (16 * g + head < heads) {
+                float all = tops[0][head];
+#pragma unroll
+                for (int w = 1; w < kPagedWaves; ++w) all = fmaxf(all, tops[w][head]);
+                float total = 0.f, y[kChannels] = {};
+#pragma unroll
+                for (int w = 0; w < kPagedWaves; ++w) {
+                    const float f = __builtin_amdgcn_exp2f(tops[w][head] - (all == -INFINITY ? 0.f : all));
+                    total = __builtin_fmaf(sums[w][head], f, total);
+#pragma unroll
+                    for (int e = 0; e < kChannels; ++e) y[e] = __builtin_fmaf(part[w][head][(who & 15) * kChannels + e], f, y[e]);
+                }
+                if (whole) {
+                    const int64_t at = (int64_t)row * a.h_q + head0 + 16 * g + head;
+                    const float inverse = 1.f / total;
+                    char* const to = a.out + at * (D * Elem<T>::kBytes);
+#pragma unroll
+                    for (int e = 0; e < kChannels; ++e) store_elem<T>(to, (who & 15) * kChannels + e, total == 0.f ? 0.f : y[e] * inverse);
+                    if (a.lse && (who & 15) == 0) a.lse[at] = (all + __builtin_log2f(total)) * 0.69314718055994530942f;
+                } else {
+                    const int64_t at = (piece * a.row_tiles + tile) * a.heads + 16 * g + head;
+#pragma unroll
+                    for (int e = 0; e < kChannels; e += 4)
+                        *reinterpret_cast<f32x4_t*>(a.part_out + at * D + (who & 15) * kChannels + e) = f32x4_t{y[e], y[e + 1], y[e + 2], y[e + 3]};
+                    if ((who & 15) == 0) *reinterpret_cast<float2*>(a.part_sum + at * 2) = float2{all, total};
+                }
             }
         }
         if (SHARES && kv == a.h_kv - 1 && x == before[s + 1] * a.h_kv) ++s;
@@ -574,7 +610,7 @@ __global__ void __launch_bounds__(256) swa_paged_join_chunks_kernel(PagedArgs a)
     constexpr int kLanes = D / 4, kTeams = 256 / kLanes;
     const int s = blockIdx.x / a.h_q, hq = blockIdx.x - s * a.h_q, tid = threadIdx.x, team = tid / kLanes, lane = tid % kLanes;
     const int kv = hq / a.group, of = hq - kv * a.group;
-    const int64_t stride = a.row_tiles * a.heads, first = ((int64_t)s * a.h_kv + kv) * a.ranges * stride + (of >> 4) * a.heads + (of & 15);
+    const int64_t stride = a.row_tiles * a.heads, first = ((int64_t)s * a.h_kv + kv) * a.ranges * stride + (of / a.tile_heads) * a.heads + of % a.tile_heads;
     __shared__ float weight[kPagedChunks], waves[4], waves2[4];
     __shared__ f32x4_t part[kTeams][kLanes];
     // (what may turn out not to be a chunk's is loaded all the same, while the length is on its way)
@@ -623,7 +659,7 @@ __global__ void __launch_bounds__(256) swa_paged_join_shares_kernel(PagedArgs a,
     if (unit.x == 0) return;
     const int kv = unit.x - 1, row = unit.y, count = unit.z, tile = rest / blocks, tid = threadIdx.x, team = tid / kLanes, lane = tid % kLanes,
               mates = kTeams / per, mate = team % mates, head = (rest - tile * blocks) * per + team / mates;
-    const bool there = head < a.heads && 16 * tile + head < a.group;
+    const bool there = head < a.heads && a.tile_heads * tile + head < a.group;
     // the share's second piece, and then the first ones of the shares behind it
     auto at = [&](int i) { return ((int64_t)(2 * (share + i) + (i == 0)) * a.row_tiles + tile) * a.heads + head; };
     float top = -INFINITY;
@@ -656,7 +692,7 @@ __global__ void __launch_bounds__(256) swa_paged_join_shares_kernel(PagedArgs a,
         y += part[team + i][lane];
         total += sums[team + i];
     }
-    const int64_t to = (int64_t)row * a.h_q + (int64_t)kv * a.group + 16 * tile + head;
+    const int64_t to = (int64_t)row * a.h_q + (int64_t)kv * a.group + a.tile_heads * tile + head;
     const float inverse = 1.f / total;
 #pragma unroll
     for (int i = 0; i < 4; ++i) store_elem<T>(a.out + to * (D * Elem<T>::kBytes), lane * 4 + i, total == 0.f ? 0.f : y[i] * inverse);
@@ -668,8 +704,10 @@ static void launch_paged_form(const PagedArgs& a, bool in_shares, hipStream_t st
 {
     const int64_t units = (int64_t)a.b * a.h_kv, works = (in_shares ? a.ranges : units * a.ranges);
     const dim3 grid((unsigned)((works + 7) / 8 * 8 * a.row_tiles)), block(64 * kPagedWaves);
-    if (in_shares) launch_kernel(swa_paged_decode_kernel<T, C, D, true>, grid, block, sizeof(int) * ((size_t)a.b + 1), stream, a);
-    else launch_kernel(swa_paged_decode_kernel<T, C, D, false>, grid, block, 0, stream, a);
+    const bool one = a.tile_heads == 16;
+    auto kernel = in_shares ? (one ? swa_paged_decode_kernel<T, C, D, true, 1> : swa_paged_decode_kernel<T, C, D, true, 2>)
+                            : (one ? swa_paged_decode_kernel<T, C, D, false, 1> : swa_paged_decode_kernel<T, C, D, false, 2>);
+    launch_kernel(kernel, grid, block, in_shares ? sizeof(int) * ((size_t)a.b + 1) : 0, stream, a);
     if (a.ranges == 1) return;
     if (!in_shares) {
         launch_kernel(swa_paged_join_chunks_kernel<T, D>, dim3((unsigned)((int64_t)a.b * a.h_q)), dim3(256), 0, stream, a);
@@ -709,7 +747,8 @@ int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_
     a.len_max = p.max_pages * p.page_size;
     if (p.len_bound > 0 && p.len_bound < a.len_max) a.len_max = p.len_bound;
     a.group = p.h_q / p.h_kv;
-    a.row_tiles = (a.group + 15) / 16;
+    a.tile_heads = tile_heads_of(p);
+    a.row_tiles = row_tiles_of(p);
     page_divisor(p.page_size, a.page_mul, a.page_shift);
     a.sixteens = p.page_size % 16 == 0;
     a.scale = (p.scale > 0.f ? p.scale : 1.f / sqrtf((float)p.d)) * 1.44269504088896340736f;
@@ -718,7 +757,7 @@ int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_
     const int64_t span = paged_span(p);
     const int64_t steps = units * ((span + kPagedStep - 1) / kPagedStep);
     if (steps > 0x7fffffffLL) return SWA_ERR_CAPACITY;
-    a.heads = a.group < 16 ? a.group : 16;
+    a.heads = a.group < a.tile_heads ? a.group : a.tile_heads;
     const bool in_shares = paged_in_shares(p);
     if (in_shares) {
         a.ranges = paged_max_shares(p);

@@ -368,6 +368,17 @@ def test_attention_over_codes(B, dtype, d, page):
 def test_heads_that_share_keys(B, h_q, h_kv, dtype):
     check_decode(B, [7, 200, 1, 77], h_q, h_kv, 64, TYPES[dtype], 16)
     check_decode(B, [130, 33], h_q, h_kv, 128, TYPES[dtype], 16)
+    if dtype == "bf16":
+        check_decode(B, [130, 33, 1], h_q, h_kv, 128, torch.float16, 16, int8=True)
+        check_decode(B, [130, 33, 1], h_q, h_kv, 64, torch.float16, 5)
+
+
+@pytest.mark.parametrize("dtype,int8", [("f32", False), ("f16", False), ("bf16", True)])
+def test_many_heads_over_long_caches(B, dtype, int8):
+    """More query heads than a workgroup has, in chunks and in shares."""
+    for d in (64, 128):
+        check_decode(B, [3000, 77, 0, 1500], 71, 1, d, TYPES[dtype], 16, int8=int8)
+        check_decode(B, [2000, 7, 0, 1100] * 8, 80, 2, d, TYPES[dtype], 16, int8=int8, len_bound=2000)
 
 
 @pytest.mark.parametrize("page", [1, 3, 16, 48, 128, 1024])
@@ -429,6 +440,12 @@ def test_pages_outside_the_pool_are_left_out(B):
 def test_values_that_are_not_finite(B):
     """Infinite values of tokens that are seen reach the output as the formula says, in their head and channel only; keys that give
     a logit of -inf count nothing, also where a whole sequence has no other."""
+    def no_key(k, v, q, table):
+        k[table[0, 0].item(), 1, 3, 5] = math.nan            # its head's two query heads, nothing else
+    for dtype in (torch.float32, torch.bfloat16, torch.float16):
+        check_decode(B, [20, 4000], 4, 2, 64, dtype, 16, edit=no_key)
+        check_decode(B, [20, 4000] * 20, 4, 2, 64, dtype, 16, edit=no_key)
+
     def infinite_value(k, v, q, table):
         v[table[0, 0].item(), 0, 3, 5] = math.inf
         v[table[1, 1].item(), 1, 2, 9] = math.nan

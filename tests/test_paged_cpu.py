@@ -150,6 +150,11 @@ def test_sizes_and_places_are_refused(B):
         assert append(B, p, **{n: ok + 8}) == B.SWA_ERR_ALIGNMENT, n
     for n in ("k_pages", "v_pages", "out", "workspace"):
         assert decode(B, p, **{n: ok + 8}) == B.SWA_ERR_ALIGNMENT, n
+    assert plan(B, p, new_cnt=ok + 0x2000) == B.SWA_ERR_BAD_SHAPE        # (the new lengths' place)
+    q8 = params(B, flags=B.SWA_KV_INT8)
+    for n in ("k_scale", "v_scale"):
+        assert append(B, q8, **{n: ok + 8}) == B.SWA_ERR_ALIGNMENT and decode(B, q8, **{n: ok + 8}) == B.SWA_ERR_ALIGNMENT, n
+        assert append(B, p, **{n: ok + 8, "slot": None}) == B.SWA_ERR_NULL               # (not looked at without codes)
     rows = [R(ok, 512), R(ok, 128), R(ok, 128)]
     assert append(B, p, rows=rows, q_out=ok) == B.SWA_ERR_BAD_SHAPE      # in place, but with gaps between the rows
 
