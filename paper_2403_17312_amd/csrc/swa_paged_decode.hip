@@ -662,36 +662,32 @@ __global__ void __launch_bounds__(256) swa_paged_join_shares_kernel(PagedArgs a,
     const bool there = head < a.heads && a.tile_heads * tile + head < a.group;
     // the share's second piece, and then the first ones of the shares behind it
     auto at = [&](int i) { return ((int64_t)(2 * (share + i) + (i == 0)) * a.row_tiles + tile) * a.heads + head; };
-    float top = -INFINITY;
-    if (there)
-        for (int i = mate * kLanes + lane; i < count; i += mates * kLanes) top = fmaxf(top, a.part_sum[at(i) * 2]);
-#pragma unroll
-    for (int o = 1; o < kLanes; o <<= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    __shared__ float tops[kTeams], sums[kTeams];
-    __shared__ f32x4_t part[kTeams][kLanes];
-    if (lane == 0) tops[team] = top;
-    __syncthreads();
-    for (int i = 0; i < mates; ++i) top = fmaxf(top, tops[team - mate + i]);
-    const float from = top == -INFINITY ? 0.f : top;
+    float top = -INFINITY, total = 0.f;
     f32x4_t y = {0.f, 0.f, 0.f, 0.f};
-    float total = 0.f;
+    auto join = [&](float most, float part_total, const f32x4_t& part_y) {
+        const float to = fmaxf(top, most), from = to == -INFINITY ? 0.f : to;
+        const float old = __builtin_amdgcn_exp2f(top - from), w = __builtin_amdgcn_exp2f(most - from);
+        y = y * old + part_y * w;
+        total = total * old + part_total * w;
+        top = to;
+    };
     if (there) {
 #pragma unroll 4
         for (int i = mate; i < count; i += mates) {
             const float2 m = *reinterpret_cast<const float2*>(a.part_sum + at(i) * 2);
-            const float w = __builtin_amdgcn_exp2f(m.x - from);
-            y += *reinterpret_cast<const f32x4_t*>(a.part_out + at(i) * D + lane * 4) * w;
-            total = __builtin_fmaf(m.y, w, total);
+            join(m.x, m.y, *reinterpret_cast<const f32x4_t*>(a.part_out + at(i) * D + lane * 4));
         }
     }
+    __shared__ float tops[kTeams], sums[kTeams];
+    __shared__ f32x4_t part[kTeams][kLanes];
     part[team][lane] = y;
-    if (lane == 0) sums[team] = total;
+    if (lane == 0) {
+        tops[team] = top;
+        sums[team] = total;
+    }
     __syncthreads();
     if (mate || !there) return;
-    for (int i = 1; i < mates; ++i) {
-        y += part[team + i][lane];
-        total += sums[team + i];
-    }
+    for (int i = 1; i < mates; ++i) join(tops[team + i], sums[team + i], part[team + i][lane]);
     const int64_t to = (int64_t)row * a.h_q + (int64_t)kv * a.group + a.tile_heads * tile + head;
     const float inverse = 1.f / total;
 #pragma unroll
