@@ -179,7 +179,7 @@ int swa_workspace_init(const swa_params *params, void *workspace, void *stream);
  * *status_out = SWA_OK, SWA_ERR_CAPACITY (some step met a full cache), SWA_ERR_HOST_STORE_FULL or
  * SWA_ERR_BAD_REQUEST (offload tier), the first of these that applies.
  * workspace == NULL reads the status word of swa_decode_step_static on the current device.
- * This is the only entry point that blocks. */
+ * This and swa_paged_check_status are the only entry points that block. */
 int swa_check_status(const swa_params *params, void *workspace, void *stream, int32_t *status_out);
 
 /*
@@ -508,6 +508,7 @@ int swa_paged_check_status(const swa_paged_params *params, void *workspace, void
  *      sequences and behind the last one.  new_len[s] = cache_len[s] + new_cnt[s].
  *   5. new_cnt[s] < 0: the sequence has finished.  Its pages go to the ring's end (in the order of sequences and pages, for
  *      the next call), new_len[s] = 0.
+ * A page belongs to one sequence: a page that two rows of the table name is handed back by both.
  * A cache_len above max_pages * page_size, and a page number outside the pool in the ring or in a finished sequence's row, set
  * the SWA_ERR_BAD_REQUEST bit; such a sequence is left alone, such a page gets slot -1.
  *   new_cnt, cache_len [b] (in); new_len [b], row_start [b+1], slot, pos [max_rows], free_state_out [2] (out);

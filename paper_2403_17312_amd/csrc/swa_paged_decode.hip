@@ -38,7 +38,7 @@ struct PagedArgs {
     int32_t b, n_rows, h_q, h_kv, page_size, n_pages, max_pages, window, len_max;
     int32_t group, row_tiles, heads, tile_heads;   // query heads of a key head, tiles of them, heads of a tile that there are at most, and that fit
     int32_t ranges;                                // shares, or chunks of a sequence at most
-    int32_t chunk;                                 // tokens; 0: the longest sequence says
+    int32_t chunk;                                 // tokens of one; 0: the longest sequence says
     uint32_t page_mul;                             // t / page_size = t * page_mul >> page_shift for 0 <= t < 2^31
     int32_t page_shift;
     int32_t sixteens;                              // pages are whole sixteens of tokens
@@ -75,8 +75,8 @@ static int64_t paged_units(const swa_paged_params& p) { return (int64_t)p.b * p.
 constexpr bool paged_two(int row_bytes, int rows, int d) { return row_bytes == 512 || (rows == 2 && d == 128); }
 
 // Shares of a call at most: the workgroups that the chip holds at once.  A CU has four of 64 channels in 16 bits, three of 64 in fp32 and of 128 (168
-// registers a lane), two of 128 in fp32 and of 128 with 32 heads, which do not fit those (64 sequences of 4352 tokens, 8 key heads: three with spills 381 us, two 356).  768 / 1024 shares of 128
-// channels: the ragged 128 sequences below 345 / 387 us; 64 of 100..8001 tokens in 8 bits 107 / 123.
+// registers a lane), two of 128 in fp32 and of 128 with 32 heads, which do not fit those (64 sequences of 4352 tokens, 8 key heads, fp32: three with
+// spills 381 us, two 356).  768 / 1024 shares of 128 channels: the ragged 128 sequences above 345 / 387 us; 64 of 100..8001 tokens in 8 bits 107 / 123.
 static int paged_max_shares(const swa_paged_params& p)
 {
     const bool two = paged_two(paged_row_bytes(p), tile_heads_of(p) / 16, p.d);
@@ -159,22 +159,26 @@ __device__ __forceinline__ int paged_sequence(const PagedArgs& a, int s, int& ro
     return tokens > kPagedStep ? (tokens + kPagedStep - 1) / kPagedStep : 1;
 }
 
-// Tokens of a chunk: a sequence has a.ranges chunks at most.  Where the caller states no bound, a table may be far wider than the lengths, and the longest of
-// those says (a microsecond of every call; 64 sequences, a wave's lanes, at most).
-__device__ __forceinline__ int paged_chunk(const PagedArgs& a)
+// Tokens of a chunk: a sequence has a.ranges chunks at most.  A bound or a table may be far above the lengths, so where its chunks were over 1024 tokens, or
+// no bound is stated, the longest sequence says (of 64 at most, a wave's lanes), which takes 0.7 to 1.6 us.  `tokens`: of the sequence that is asked for.
+__device__ __forceinline__ int paged_chunk(const PagedArgs& a, int tokens)
 {
     if (a.chunk) return a.chunk;
-    const int lane = threadIdx.x & 63;
-    int row, lo = 0, n = 0, tokens = 1;
-    bool too_long = false;
-    if (lane < a.b && paged_sequence(a, lane, row, lo, n, too_long)) tokens = n - (lo & ~31);
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-        const int other = __shfl_xor(tokens, o, 64);
-        tokens = tokens > other ? tokens : other;
+    if (a.b > 1) {
+        const int lane = threadIdx.x & 63;
+        int row, lo = 0, n = 0;
+        bool too_long = false;
+        if (lane < a.b && paged_sequence(a, lane, row, lo, n, too_long)) tokens = n - (lo & ~31);
+        auto larger = [](int x, int y) { return x > y ? x : y; };
+        tokens = larger(tokens, __builtin_amdgcn_update_dpp(0, tokens, 0xB1, 0xf, 0xf, true));    // within rows of 16 lanes
+        tokens = larger(tokens, __builtin_amdgcn_update_dpp(0, tokens, 0x4E, 0xf, 0xf, true));
+        tokens = larger(tokens, __builtin_amdgcn_update_dpp(0, tokens, 0x141, 0xf, 0xf, true));
+        tokens = larger(tokens, __builtin_amdgcn_update_dpp(0, tokens, 0x140, 0xf, 0xf, true));
+        tokens = larger(tokens, __shfl_xor(tokens, 16, 64));
+        tokens = larger(tokens, __shfl_xor(tokens, 32, 64));
     }
-    const int per_step = a.ranges * kPagedStep;          // (at most 2^31 / 2 and rounded up: tokens below 2^31 and 2^15 above them)
-    return __builtin_amdgcn_readfirstlane((int)(((uint32_t)(tokens < 1 ? 1 : tokens) + (uint32_t)per_step - 1) / (uint32_t)per_step)) * kPagedStep;
+    const int per_step = a.ranges * kPagedStep;
+    return __builtin_amdgcn_readfirstlane(tokens > per_step ? (tokens + per_step - 1) / per_step : 1) * kPagedStep;
 }
 
 // The shares: the first `more` of them have one step more than the others.
@@ -286,7 +290,7 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
             row = s;
             if (a.row_start) {
                 row = a.row_start[s + 1] - 1;
-                if (row < a.row_start[s] || row >= a.n_rows) return;
+                if (row < 0 || row < a.row_start[s] || row >= a.n_rows) return;
             }
         }
 
@@ -310,7 +314,7 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
                 if (too_long && split == 0 && tid == 0) atomicOr(a.status, kStatusCapacityBit);
                 return;
             }
-            const int from = lo & ~31, chunk = paged_chunk(a);
+            const int from = lo & ~31, chunk = paged_chunk(a, n - from);
             begin = from + split * chunk;
             if (split > 0 && begin >= n) return;
             end = n - begin < chunk ? n : begin + chunk;
@@ -620,8 +624,9 @@ __global__ void __launch_bounds__(256) swa_paged_join_chunks_kernel(PagedArgs a)
     if (ahead && team < a.ranges) y = *reinterpret_cast<const f32x4_t*>(a.part_out + (first + team * stride) * D + lane * 4);
     int row, lo, n;
     bool too_long;
-    const int chunk = paged_chunk(a);
-    if (!paged_sequence(a, s, row, lo, n, too_long) || n - (lo & ~31) <= chunk) return;
+    if (!paged_sequence(a, s, row, lo, n, too_long)) return;
+    const int chunk = paged_chunk(a, n - (lo & ~31));
+    if (n - (lo & ~31) <= chunk) return;
     const int count = (n - (lo & ~31) + chunk - 1) / chunk;
     mine = tid < count ? mine : float2{-INFINITY, 0.f};
     float top = wave_max(mine.x);
@@ -771,7 +776,7 @@ int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_
                 each = e;
             }
         }
-        a.chunk = p.len_bound > 0 || p.b > 64 ? (int32_t)(each * kPagedStep) : 0;
+        a.chunk = (p.len_bound > 0 && each <= 8) || p.b > 64 ? (int32_t)(each * kPagedStep) : 0;
         a.ranges = (int32_t)((of_one + each - 1) / each);
     }
     a.part_out = reinterpret_cast<float*>(static_cast<char*>(workspace) + kPagedPartialOffset);
