@@ -328,7 +328,7 @@ def check_decode(B, lens, h_q, h_kv, d, dtype, page, window=0, int8=False, scale
     seen = set()
     for s, m in enumerate(lens):
         row = row_start[s + 1] - 1 if row_start else s
-        if m < 0 or s in skipped or (row_start and row < row_start[s]) or row >= n_rows:
+        if m < 0 or s in skipped or (row_start and row < row_start[s]) or not 0 <= row < n_rows:
             continue
         seen.add(row)
         lo = max(0, m - window) if window else 0
@@ -425,6 +425,9 @@ def test_padded_batches_and_rows_of_a_plan(B):
     check_decode(B, [33, -1, 90, 0, -1], 4, 2, 64, torch.bfloat16, 16)
     # sequence 1 has no new rows, sequence 2 three, sequence 4's row lies beyond the call's
     check_decode(B, [33, 50, 90, 12, 8], 4, 2, 64, torch.bfloat16, 16, row_start=[0, 1, 1, 4, 5, 6], n_rows=5)
+    # rows that no plan gives
+    check_decode(B, [33, 50, 90], 4, 2, 64, torch.bfloat16, 16, row_start=[-5, -1, 1, 2 ** 30], n_rows=3)
+    check_decode(B, [1500, 50, 90] * 12, 4, 2, 64, torch.bfloat16, 16, row_start=[-5, -1, 1] + [2 ** 30] * 34, n_rows=3)
 
 
 def test_sequences_beyond_the_bound_are_skipped(B):
