@@ -1,8 +1,8 @@
 // Attention of one new token per sequence over a paged cache.  Bound by HBM: every key and value of the window is read once, 4 flops for
 // two elements and query head.
 //
-// A workgroup serves up to 16 (or 32) of the query heads that share a key head, over a range of one sequence's tokens; its four waves take tiles of the range
-// in turn, each with a running maximum and sum of the softmax.  Ranges come in two ways:
+// A workgroup serves up to 16 (or 32) of the query heads that share a key head, over a range of one sequence's tokens; its four waves (one where
+// sequences are short) take tiles of the range in turn, each with a running maximum and sum of the softmax.  Ranges come in two ways:
 //   chunks   few sequences: each one's tokens in equal chunks, as many as fill the CUs evenly, a workgroup for each.
 //   shares   many, and long ones: the call's work, in steps of 128 tokens of one sequence and key head, laid end to end and cut into as
 //            many equal shares as there are workgroups, whatever the lengths are; each workgroup sums the lengths up by itself.  A share
@@ -38,6 +38,7 @@ struct PagedArgs {
     int32_t b, n_rows, h_q, h_kv, page_size, n_pages, max_pages, window, len_max;
     int32_t group, row_tiles, heads, tile_heads;   // query heads of a key head, tiles of them, heads of a tile that there are at most, and that fit
     int32_t ranges;                                // shares, or chunks of a sequence at most
+    int32_t span;                                  // tokens of a sequence that the call may see
     int32_t chunk;                                 // tokens of one; 0: the longest sequence says
     uint32_t page_mul;                             // t / page_size = t * page_mul >> page_shift for 0 <= t < 2^31
     int32_t page_shift;
@@ -62,12 +63,16 @@ static int64_t paged_span(const swa_paged_params& p)
     return p.window > 0 && p.window < n ? (int64_t)p.window + 31 : n;
 }
 
-// Shares take a launch's time longer to begin (the sums) and to end (pieces), and level the lengths out.  us, chunks / shares, 32 query and 8 key
-// heads of 128 bf16 channels, lengths even over 100..8001, and all 4000: 4 sequences 25.9 / 27.4, 19.7 / 19.9; 8: 33.3 / 32.0, 28.6 / 31.4; 16: 58.8 / 53.7, 47.9 /
-// 50.5; 32: 113 / 95, 87 / 90; 64: 217 / 178, 174 / 176; 128: 398 / 345, 331 / 338.  16 sequences of 32 fp32 heads, 64 channels, a window of 512: 27.2 / 30.5.
+// Shares take about two microseconds longer (the sums, and pieces to join), and level the lengths out.  us, chunks / shares, 128 bf16 channels, lengths even
+// over 100..8001 and all 4000, 32 query and 8 key heads: 8 sequences 33.3 / 32.0, 28.6 / 31.4; 16: 58.8 / 53.7, 47.9 / 50.5; 32: 113 / 95, 87 / 90; 64: 217 / 178,
+// 174 / 176; 128: 398 / 345, 331 / 338.  Fewer pairs want more tokens; lengths 1..n and all n: 2 of 16000 24.9 / 22.9, 28.5 / 31.6, of 64000 73.9 / 50, 88 / 89;
+// 6 of 4000 21.0 / 20.3, 24.1 / 27.3, of 16000 56.6 / 41, 68 / 71; one key head, 32 of 16000 41.5 / 37.5, 49.9 / 57, 16 of 16000 25.5 / 27.4.  One sequence has
+// nothing to level.  16 sequences of 32 fp32 heads, 64 channels, a window of 512: 27.2 / 30.5.
 static bool paged_in_shares(const swa_paged_params& p)
 {
-    return (int64_t)p.b * p.h_kv * row_tiles_of(p) >= 64 && paged_span(p) >= 1024;
+    if (paged_span(p) < 1024) return false;
+    const int64_t pairs = (int64_t)p.b * p.h_kv;
+    return pairs * row_tiles_of(p) >= 64 || (p.b > 1 && pairs * paged_span(p) * 2 * paged_row_bytes(p) >= (240 << 20));
 }
 
 static int64_t paged_units(const swa_paged_params& p) { return (int64_t)p.b * p.h_kv * row_tiles_of(p); }
@@ -97,7 +102,7 @@ static int64_t paged_piece_rows(const swa_paged_params& p)
     const int group = p.h_q / p.h_kv;
     const int64_t shares = 2 * (int64_t)paged_max_shares(p) * row_tiles_of(p);
     const int64_t chunks = paged_chunks(p, 3) > 1 ? paged_chunks(p, 3) * paged_units(p) : 0;
-    const int64_t pieces = paged_units(p) >= 64 && shares > chunks ? shares : chunks;
+    const int64_t pieces = (paged_units(p) >= 64 || p.b > 1) && shares > chunks ? shares : chunks;
     return 2 * ((pieces * (group < tile_heads_of(p) ? group : tile_heads_of(p)) + 1) / 2);
 }
 
@@ -193,8 +198,8 @@ struct Shares {
 };
 
 // T: type of queries and outputs, C: of the pages (Q8: codes).
-template <typename T, typename C, int D, bool SHARES, int ROWS>
-__global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * D, ROWS, D) ? 2 : 3) swa_paged_decode_kernel(PagedArgs a)
+template <typename T, typename C, int D, bool SHARES, int ROWS, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, paged_two(Elem<C>::kBytes * D, ROWS, D) ? 2 : 3) swa_paged_decode_kernel(PagedArgs a)
 {
     constexpr bool kCodes = std::is_same_v<C, Q8>, kWide = std::is_same_v<C, F32>;
     // Codes are exact in either 16-bit type.  Keys get the queries' type; values get bf16, whose range the weights need, which are products with a
@@ -209,8 +214,8 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
     const int heads = a.group - 16 * ROWS * tile < 16 * ROWS ? a.group - 16 * ROWS * tile : 16 * ROWS;
 
     constexpr int kPitch = D + 4;
-    __shared__ float part[kPagedWaves][16][kPitch];
-    __shared__ float tops[kPagedWaves][16], sums[kPagedWaves][16];
+    __shared__ float part[WAVES][16][kPitch];
+    __shared__ float tops[WAVES][16], sums[WAVES][16];
     extern __shared__ int before[];                      // shares: steps of a key head before sequence s, for s <= b
 
     int s = 0, kv = 0, row, lo, n, split = 0, x = 0, x1 = 0;
@@ -221,8 +226,8 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
     int early_page = 0;
     if constexpr (SHARES) {
         if (work >= a.ranges) return;
-        __shared__ int wave_steps[kPagedWaves];
-        const int per = (a.b + 64 * kPagedWaves - 1) / (64 * kPagedWaves), s0 = tid * per, s1 = s0 + per < a.b ? s0 + per : a.b;
+        __shared__ int wave_steps[WAVES];
+        const int per = (a.b + 64 * WAVES - 1) / (64 * WAVES), s0 = tid * per, s1 = s0 + per < a.b ? s0 + per : a.b;
         int own = 0;
         for (int i = s0; i < s1; ++i) {
             own += paged_sequence(a, i, row, lo, n, too_long);
@@ -513,7 +518,7 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
 
         // Whole tiles first; the others, at the ends of the window and where a page is not in the pool, in a loop of their own, whose addresses then
         // take no registers from this one.
-        constexpr int kStride = kPagedWaves * kKeys;
+        constexpr int kStride = WAVES * kKeys;
         // The pool's rows of a tile's tokens, -1 where there is none.
         auto row_of = [&](int base, int page) {
             const int t = base + (lane & (kKeys - 1));
@@ -573,14 +578,13 @@ __global__ void __launch_bounds__(64 * kPagedWaves, paged_two(Elem<C>::kBytes * 
 #pragma unroll
                 for (int i = 0; i < 4; ++i) part[wave][to_col][kWide ? (e / 4) * 64 + (4 * to_j + i) * 4 + e % 4 : (4 * to_j + i) * kChannels + e] = acc[g][e][i];
             __syncthreads();
-            const int head = who >> 4;
-            if (16 * g + head < heads) {
+            for (int head = who >> 4; head < 16 && 16 * g + head < heads; head += 4 * WAVES) {
                 float all = tops[0][head];
 #pragma unroll
-                for (int w = 1; w < kPagedWaves; ++w) all = fmaxf(all, tops[w][head]);
+                for (int w = 1; w < WAVES; ++w) all = fmaxf(all, tops[w][head]);
                 float total = 0.f, y[kChannels] = {};
 #pragma unroll
-                for (int w = 0; w < kPagedWaves; ++w) {
+                for (int w = 0; w < WAVES; ++w) {
                     const float f = __builtin_amdgcn_exp2f(tops[w][head] - (all == -INFINITY ? 0.f : all));
                     total = __builtin_fmaf(sums[w][head], f, total);
 #pragma unroll
@@ -704,18 +708,24 @@ template <typename T, typename C, int D>
 static void launch_paged_form(const PagedArgs& a, bool in_shares, hipStream_t stream)
 {
     const int64_t units = (int64_t)a.b * a.h_kv, works = (in_shares ? a.ranges : units * a.ranges);
-    const dim3 grid((unsigned)((works + 7) / 8 * 8 * a.row_tiles)), block(64 * kPagedWaves);
-    const bool one = a.tile_heads == 16;
-    auto kernel = in_shares ? (one ? swa_paged_decode_kernel<T, C, D, true, 1> : swa_paged_decode_kernel<T, C, D, true, 2>)
-                            : (one ? swa_paged_decode_kernel<T, C, D, false, 1> : swa_paged_decode_kernel<T, C, D, false, 2>);
-    launch_kernel(kernel, grid, block, in_shares ? sizeof(int) * ((size_t)a.b + 1) : 0, stream, a);
+    const dim3 grid((unsigned)((works + 7) / 8 * 8 * a.row_tiles));
+    // Short sequences have work for one wave, and many of them more workgroups than four waves leave places for: us with four / one, lengths 1..n and all n,
+    // bf16, d = 128, 32 key heads: 256 sequences n = 16 39.5 / 17.3, 41 / 20, n = 128 60.5 / 49.2, 91 / 86; 64 n = 32 12.2 / 7.8, 12.8 / 9.4, n = 256 28.1 / 26.8,
+    // 45.5 / 44.3, n = 512 48.5 / 49.9, 84 / 84; 32 n = 128 11.9 / 10.7, 14.9 / 14.9, n = 256 17.1 / 18.1, 24.8 / 26.1.
+    const int64_t all = units * a.row_tiles;
+    const bool one = a.tile_heads == 16,
+               single = !in_shares && a.ranges == 1 && (a.span <= 32 || (all >= 1024 && a.span <= 128) || (all >= 2048 && a.span <= 256));
+    auto kernel = in_shares ? (one ? swa_paged_decode_kernel<T, C, D, true, 1, 4> : swa_paged_decode_kernel<T, C, D, true, 2, 4>)
+                  : single  ? (one ? swa_paged_decode_kernel<T, C, D, false, 1, 1> : swa_paged_decode_kernel<T, C, D, false, 2, 1>)
+                            : (one ? swa_paged_decode_kernel<T, C, D, false, 1, 4> : swa_paged_decode_kernel<T, C, D, false, 2, 4>);
+    launch_kernel(kernel, grid, dim3(single ? 64 : 64 * kPagedWaves), in_shares ? sizeof(int) * ((size_t)a.b + 1) : 0, stream, a);
     if (a.ranges == 1) return;
     if (!in_shares) {
         launch_kernel(swa_paged_join_chunks_kernel<T, D>, dim3((unsigned)((int64_t)a.b * a.h_q)), dim3(256), 0, stream, a);
         return;
     }
-    int per = 1;                                         // (few pieces of a sequence: a workgroup joins several heads)
-    while (per < 1024 / D && per < a.heads) per *= 2;
+    int per = 1;                                         // (where a sequence has few pieces, a workgroup joins several heads)
+    while (per < 1024 / D && per < a.heads && a.ranges < 4 * units * per) per *= 2;
     launch_kernel(swa_paged_join_shares_kernel<T, D>, dim3((unsigned)((int64_t)a.ranges * a.row_tiles * ((a.heads + per - 1) / per))), dim3(256), 0,
                   stream, a, per);
 }
@@ -756,6 +766,7 @@ int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_
 
     const int64_t units = (int64_t)p.b * p.h_kv;
     const int64_t span = paged_span(p);
+    a.span = (int32_t)span;
     const int64_t steps = units * ((span + kPagedStep - 1) / kPagedStep);
     if (steps > 0x7fffffffLL) return SWA_ERR_CAPACITY;
     a.heads = a.group < a.tile_heads ? a.group : a.tile_heads;

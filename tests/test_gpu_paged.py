@@ -409,6 +409,24 @@ def test_many_sequences(B):
     check_decode(B, [rng.randrange(0, 60) for _ in range(1500)], 2, 1, 64, torch.float16, 16, len_bound=60)
 
 
+@pytest.mark.parametrize("dtype,int8", [("f32", False), ("bf16", False), ("f16", True)])
+def test_short_sequences_by_one_wave(B, dtype, int8):
+    """Up to 32 tokens, and up to 128 and 256 of many sequences and heads; the same with more query heads than a wave's threads join at once."""
+    rng = random.Random(4)
+    for d in (64, 128):
+        check_decode(B, [0, 1, 31, 32, 17, -1], 7, 7, d, TYPES[dtype], 16, int8=int8)
+        check_decode(B, [0, 1, 31, 32, 17], 32, 2, d, TYPES[dtype], 3, int8=int8)
+        check_decode(B, [0, 1, 31, 32, 17], 37, 1, d, TYPES[dtype], 16, int8=int8)
+    check_decode(B, [rng.randrange(0, 129) for _ in range(64)], 32, 16, 64, TYPES[dtype], 16, int8=int8)
+    check_decode(B, [rng.randrange(0, 257) for _ in range(128)], 16, 16, 64, TYPES[dtype], 16, int8=int8)
+    check_decode(B, [rng.randrange(0, 500) for _ in range(64)], 16, 16, 64, TYPES[dtype], 16, int8=int8, window=90)
+
+
+@pytest.mark.parametrize("dtype,int8", [("bf16", False), ("f16", True)])
+def test_few_long_sequences_in_shares(B, dtype, int8):
+    check_decode(B, [70000, 3, 20001], 16, 8, 128, TYPES[dtype], 64, int8=int8)
+
+
 def test_queries_sharp_and_scales(B):
     for dtype in (torch.float32, torch.bfloat16):
         check_decode(B, [300, 64], 4, 2, 128, dtype, 16, loud=20.0)
