@@ -778,11 +778,14 @@ int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_
         // Work is even, so a call takes as long as the CU that has most of it.  us, as many chunks as make 1024 workgroups, 512, and by this rule (two
         // on a CU before three before one): 131071 tokens, 4 key heads, 16 query heads each 54.5 / 50.4 / 50.4; 6 sequences of 32000, 8 key heads 126.8 /
         // 155 (some CUs three) / 126.4; 2 of 10000, fp32 37.9 / 36.3 / 32.3.
-        int64_t least = INT64_MAX, each = of_one;        // steps of that CU, and of a workgroup
+        // And the join, whose launch is worth about a step (2 us), and another one with a thousand query heads to join: us, by these chunks without that / one
+        // chunk, fp16, d = 128: 1 sequence, 8 key heads, 256 tokens 7.4 / 6.2, 384 7.5 / 7.8, 1000 8.3 / 20.2; 183 sequences of 16 query heads on one, 256 13.7 /
+        // 8.2, 1000 23.1 / 20.1; 48 of 64 on 8, 512 21.8 / 17.9, 1000 32.5 / 30.9.
+        int64_t each = of_one, least = (paged_units(p) + 255) / 256 * of_one * 1024;     // steps of a workgroup; of that CU, in 1024ths
         for (int k : {2, 3, 1}) {
             const int64_t e = (of_one + paged_chunks(p, k) - 1) / paged_chunks(p, k), groups = paged_units(p) * ((of_one + e - 1) / e);
-            const int64_t most = (groups + 255) / 256 * e;
-            if (most < least) {
+            const int64_t most = (groups + 255) / 256 * e * 1024 + 1024 + (int64_t)p.b * p.h_q;
+            if (e < of_one && most < least) {
                 least = most;
                 each = e;
             }
