@@ -497,6 +497,12 @@ def test_logits_of_minus_infinity(B, dtype):
     assert ((out[0, :2].cpu().double() - want).abs() <= tol).all() and ((lse[0, :2].cpu().double() - want_lse).abs() <= lse_tol).all()
 
 
+def test_a_million_tokens_and_the_most_sequences(B):
+    check_decode(B, [1 << 20], 1, 1, 64, torch.bfloat16, 16, len_bound=1 << 20)
+    check_decode(B, [1] * 4095 + [40], 2, 1, 64, torch.bfloat16, 16)
+    check_decode(B, [3] * 4094 + [2000, 40], 2, 1, 64, torch.float16, 16)
+
+
 def test_offsets_beyond_32_bits(B):
     """A pool of 2^25 rows of 256 bytes: the last pages begin 2^33 bytes and 2^32 elements in."""
     n_pages, page, d = (1 << 25) // 16 + 40, 16, 128
