@@ -488,7 +488,7 @@ typedef struct {
 } swa_rows;
 
 /* Workspace of the paged calls, as swa_workspace_bytes, swa_workspace_init and swa_check_status are for the others.  The size
- * goes by b, the heads and d.  Calls that overlap in time need workspaces of their own. */
+ * goes by b, the heads, d and dtype.  Calls that overlap in time need workspaces of their own. */
 size_t swa_paged_workspace_bytes(const swa_paged_params *params);
 int swa_paged_workspace_init(const swa_paged_params *params, void *workspace, void *stream);
 int swa_paged_check_status(const swa_paged_params *params, void *workspace, void *stream, int32_t *status_out);

@@ -6,7 +6,8 @@
 //   chunks   few sequences: each one's tokens in equal chunks, as many as fill the CUs evenly, a workgroup for each.
 //   shares   many, and long ones: the call's work, in steps of 128 tokens of one sequence and key head, laid end to end and cut into as
 //            many equal shares as there are workgroups, whatever the lengths are; each workgroup sums the lengths up by itself.  A share
-//            holds whole sequences and at most two pieces.  128 sequences of 512 to 8192 tokens, 8 key heads of 128 bf16 channels: chunks 425 us, shares 353 (6.5 TB/s).
+//            holds whole sequences and at most two pieces.  128 sequences of 512 to 8192 tokens, 8 key heads of 128 bf16 channels: chunks
+//            425 us, shares 353 (6.5 TB/s).
 // Pieces leave partial results, which a second, small launch joins in their order.
 // All products go to the matrix cores, whose 16 columns are the query heads: also a single head's, since the matrix cores have
 // fifteen times the time that HBM leaves them.
@@ -645,7 +646,8 @@ __global__ void __launch_bounds__(256) swa_paged_join_chunks_kernel(PagedArgs a)
     const float total = (waves2[0] + waves2[1]) + (waves2[2] + waves2[3]);
     y = ahead && team < count ? y * weight[team] : f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-    for (int i = ahead ? team + kTeams : team; i < count; i += kTeams) y += *reinterpret_cast<const f32x4_t*>(a.part_out + (first + i * stride) * D + lane * 4) * weight[i];
+    for (int i = ahead ? team + kTeams : team; i < count; i += kTeams)
+        y += *reinterpret_cast<const f32x4_t*>(a.part_out + (first + i * stride) * D + lane * 4) * weight[i];
     part[team][lane] = y;
     __syncthreads();
     if (team) return;

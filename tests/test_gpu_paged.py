@@ -450,6 +450,7 @@ def test_padded_batches_and_rows_of_a_plan(B):
 
 def test_sequences_beyond_the_bound_are_skipped(B):
     check_decode(B, [33, 100, 64, 65], 4, 2, 64, torch.bfloat16, 16, len_bound=64, skipped=(1, 3))
+    check_decode(B, [33, 1300, 1200, 1201] * 10, 4, 2, 64, torch.bfloat16, 16, len_bound=1200, skipped=tuple(range(1, 40, 2)))
 
 
 def test_pages_outside_the_pool_are_left_out(B):
