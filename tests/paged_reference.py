@@ -111,5 +111,9 @@ def attention(q, k, v, scale, dtype, weight_step, query_step=0.0):
     off = 2.0 ** -24 * ((d + 8) * size.amax(-1) + 16 * spread + 32) + query_step * size.amax(-1)
     weights = (w[..., None] * vv.abs()).sum(1)
     sums = (64 + x.shape[-1] / 16) * 2.0 ** -24              # a chain of partial sums, sixteen lanes' at the least
-    tol = half_step(dtype) * out.abs() + (weight_step + 2 * off[:, None] + 2 * sums) * weights + (2.0 ** -25 if dtype == torch.float16 else 0)
+    tol = half_step(dtype) * out.abs() + (weight_step + 2 * off[:, None] + 2 * sums) * weights
+    if dtype == torch.float16:
+        # Below 2^-14 a fp16 number's half step is 2^-25 whatever its size.  So for the output; and for a weight, which is rounded relative to the
+        # largest one, 1, of those seen when it is: its share of the sum, which is at least 1, is then off by 2^-25 at most, times its value.
+        tol = tol + 2.0 ** -25 * (1 + vv.abs().sum(1))
     return out, lse, tol, off + sums + 2.0 ** -23 * lse.abs()
