@@ -546,7 +546,7 @@ int swa_paged_append(const swa_paged_params *params, swa_rows q, swa_rows k, swa
  * rows, or with a row beyond n_rows are skipped: nothing is written for them.  Where no token is left or every logit is -inf (so
  * for cache_len = 0), out = 0 and lse = -inf.
  * Accumulated in fp32; the weights are rounded to dtype (8-bit codes: to 16 bits of mantissa) for their product with the
- * values, out is rounded once.  A call's results do not depend on the order in which its workgroups run; a sequence's may differ
+ * values (relative to themselves; in fp16 those below 2^-29 of the largest lose bits, those below 2^-40 count nothing), out is rounded once.  A call's results do not depend on the order in which its workgroups run; a sequence's may differ
  * in their last bits with the call's other lengths and with len_bound, which say where its tokens are cut into pieces.
  * A sequence longer than max_pages * page_size or a stated len_bound is skipped, and the SWA_ERR_CAPACITY bit is set.  Tokens of
  * pages outside the pool are left out of the sums, and the SWA_ERR_BAD_REQUEST bit is set.
