@@ -548,6 +548,8 @@ int swa_paged_append(const swa_paged_params *params, swa_rows q, swa_rows k, swa
  * Accumulated in fp32; the weights are rounded to dtype (8-bit codes: to 16 bits of mantissa) for their product with the
  * values (relative to themselves; in fp16 those below 2^-29 of the largest lose bits, those below 2^-40 count nothing), out is rounded once.  A call's results do not depend on the order in which its workgroups run; a sequence's may differ
  * in their last bits with the call's other lengths and with len_bound, which say where its tokens are cut into pieces.
+ * A sequence that the plan refused keeps its rows in row_start and its cache_len: this call attends for it with whatever q holds
+ * there, which swa_paged_append has not written.  swa_paged_decode_planned leaves such sequences out.
  * A sequence longer than max_pages * page_size or a stated len_bound is skipped, and the SWA_ERR_CAPACITY bit is set.  Tokens of
  * pages outside the pool are left out of the sums, and the SWA_ERR_BAD_REQUEST bit is set.
  *   q [n_rows, h_q, d] (in); row_start [b+1] or NULL (then n_rows >= b); out [n_rows, h_q, d] dense, lse [n_rows, h_q] float32 or
@@ -556,6 +558,16 @@ int swa_paged_append(const swa_paged_params *params, swa_rows q, swa_rows k, swa
 int swa_paged_decode(const swa_paged_params *params, swa_rows q, int32_t n_rows, const int32_t *row_start, const void *k_pages,
                      const void *v_pages, const float *k_scale, const float *v_scale, const int32_t *block_table,
                      const int32_t *cache_len, void *out, float *lse, void *workspace, void *stream);
+
+/*
+ * swa_paged_decode for the rows of a plan: sequences whose row has a negative slot (those that the plan refused, and those whose new token's
+ * page lies outside the pool) are skipped too, nothing is written for them.
+ *   row_start [b+1], slot [n_rows] as swa_paged_plan wrote them (in).  Rows of a plan beyond n_rows are skipped, so n_rows is at
+ *   most the plan's max_rows.
+ */
+int swa_paged_decode_planned(const swa_paged_params *params, swa_rows q, int32_t n_rows, const int32_t *row_start, const int32_t *slot,
+                             const void *k_pages, const void *v_pages, const float *k_scale, const float *v_scale,
+                             const int32_t *block_table, const int32_t *cache_len, void *out, float *lse, void *workspace, void *stream);
 
 /*
  * Measurement aid, not part of the method: reads `bytes` (rounded down to a multiple of 104 KiB)

@@ -44,7 +44,8 @@ EXPORTS = ["swa_strerror", "swa_workspace_bytes", "swa_workspace_init", "swa_che
            "swa_budget", "swa_prefill_scores", "swa_decode_step", "swa_compact_kv", "swa_quantize_kv",
            "swa_decode_step_q8", "swa_prefill_rows", "swa_decode_step_window", "swa_prefill_attention", "swa_probe_stream_read",
            "swa_prepare", "swa_decode_step_static", "swa_decode_step_window_q8", "swa_offload_evicted", "swa_reload_tokens",
-           "swa_paged_workspace_bytes", "swa_paged_workspace_init", "swa_paged_check_status", "swa_paged_plan", "swa_paged_append", "swa_paged_decode"]
+           "swa_paged_workspace_bytes", "swa_paged_workspace_init", "swa_paged_check_status", "swa_paged_plan", "swa_paged_append", "swa_paged_decode",
+           "swa_paged_decode_planned"]
 
 
 class SwaParams(ctypes.Structure):
@@ -84,7 +85,7 @@ _native = None      # the native half (csrc/swa_native.cpp), bound to the entry 
 # not a plain tensor, an integer or None; the call then takes the general path below, with its errors.
 NATIVE = ("swa_decode_step", "swa_decode_step_q8", "swa_decode_step_window", "swa_decode_step_window_q8", "swa_decode_step_static",
           "swa_compact_kv", "swa_prefill_scores", "swa_prefill_rows", "swa_prefill_attention", "swa_quantize_kv",
-          "swa_paged_plan", "swa_paged_append", "swa_paged_decode")
+          "swa_paged_plan", "swa_paged_append", "swa_paged_decode", "swa_paged_decode_planned")
 
 
 class _General:
@@ -169,6 +170,8 @@ def lib():
         L.swa_paged_append.argtypes = [gp] + [SwaRows] * 3 + [ctypes.c_int32] + [vp] * 12
         L.swa_paged_decode.restype = ctypes.c_int
         L.swa_paged_decode.argtypes = [gp, SwaRows, ctypes.c_int32] + [vp] * 11
+        L.swa_paged_decode_planned.restype = ctypes.c_int
+        L.swa_paged_decode_planned.argtypes = [gp, SwaRows, ctypes.c_int32] + [vp] * 12
         _lib, _native = L, _native_half(L)
     return _lib
 
@@ -470,6 +473,18 @@ def swa_paged_decode(params: SwaPagedParams, q, n_rows: int, row_start, k_pages,
         raise SwaError(rc, "swa_paged_decode")
 
 
+def swa_paged_decode_planned(params: SwaPagedParams, q, n_rows: int, row_start, slot, k_pages, v_pages, k_scale, v_scale, block_table,
+                             cache_len, out, lse, workspace, stream=None) -> None:
+    rc = _fast().swa_paged_decode_planned(params, q, n_rows, row_start, slot, k_pages, v_pages, k_scale, v_scale, block_table, cache_len,
+        out, lse, workspace, stream)
+    if rc is None:
+        rc = lib().swa_paged_decode_planned(ctypes.byref(params), _rows(q), int(n_rows), _gpu_ptr(row_start), _gpu_ptr(slot),
+            _gpu_ptr(k_pages), _gpu_ptr(v_pages), _gpu_ptr(k_scale), _gpu_ptr(v_scale), _gpu_ptr(block_table), _gpu_ptr(cache_len),
+            _gpu_ptr(out), _gpu_ptr(lse), _gpu_ptr(workspace), _stream(stream))
+    if rc != SWA_OK:
+        raise SwaError(rc, "swa_paged_decode_planned")
+
+
 class PagedCache:
     """Device tensors of a paged cache: one pool per layer, one plan for all of them (allocation plumbing, and checks of what is
     handed in).  A step is plan(), then append() and decode() for every layer."""
@@ -493,6 +508,7 @@ class PagedCache:
         self.free_state = torch.tensor([0, p.n_pages], dtype=torch.int32, device=device)
         self._other_state = torch.zeros_like(self.free_state)
         self.row_start = torch.zeros((p.b + 1,), dtype=torch.int32, device=device)
+        self._slot = None                              # of the last plan
         self.workspace = torch.zeros((nbytes,), dtype=torch.uint8, device=device)
         swa_paged_workspace_init(p, self.workspace)
 
@@ -501,7 +517,8 @@ class PagedCache:
             raise ValueError(f"{name} must be {list(shape)} of {dtype}, this is {list(t.shape)} of {t.dtype}")
 
     def plan(self, new_cnt, slot, pos, stream=None) -> None:
-        """new_cnt [b] (-1: finished); slot and pos [rows] are filled.  cache_len counts the new tokens afterwards."""
+        """new_cnt [b] (-1: finished); slot and pos [rows] are filled.  cache_len counts the new tokens afterwards.  A sequence for which pages or
+        rows ran out is refused: its rows have slots of -1, its cache_len stays."""
         self._expect("new_cnt", new_cnt, (self.params.b,), torch.int32)
         self._expect("slot", slot, (slot.numel(),), torch.int32)
         self._expect("pos", pos, slot.shape, torch.int32)
@@ -509,6 +526,7 @@ class PagedCache:
                        self._other_state, slot.numel(), self.row_start, slot, pos, self.workspace, stream)
         self.cache_len, self._other_len = self._other_len, self.cache_len
         self.free_state, self._other_state = self._other_state, self.free_state
+        self._slot = slot
 
     def append(self, layer: int, q, k, v, slot, pos, inv_freq, q_out, q_weight=None, k_weight=None, stream=None) -> None:
         """pos [rows], or [axes, rows] with several axes."""
@@ -528,14 +546,18 @@ class PagedCache:
                          self.k_scale[layer], self.v_scale[layer], self.workspace, stream)
 
     def decode(self, layer: int, q, out, lse=None, by_rows: bool = False, stream=None) -> None:
-        """by_rows: q and out hold the plan's packed rows, and each sequence's last one is meant; otherwise row s is sequence s."""
+        """by_rows: q and out hold the plan's packed rows, and each sequence's last one is meant; nothing is written for a sequence that the plan
+        has refused (its slots, which still hold what plan() wrote, say so).  Otherwise row s is sequence s, whether it was refused or not."""
         p, n = self.params, q.shape[0]
         self._expect("q", q, (n, p.h_q, p.d), self.dtype)
         self._expect("out", out, (n, p.h_q, p.d), self.dtype)
         if lse is not None:
             self._expect("lse", lse, (n, p.h_q), torch.float32)
-        swa_paged_decode(p, q, n, self.row_start if by_rows else None, self.k_pages[layer], self.v_pages[layer], self.k_scale[layer],
-                         self.v_scale[layer], self.block_table, self.cache_len, out, lse, self.workspace, stream)
+        cache = (self.k_pages[layer], self.v_pages[layer], self.k_scale[layer], self.v_scale[layer], self.block_table, self.cache_len)
+        if by_rows and self._slot is not None:
+            swa_paged_decode_planned(p, q, min(n, self._slot.numel()), self.row_start, self._slot, *cache, out, lse, self.workspace, stream)
+        else:
+            swa_paged_decode(p, q, n, self.row_start if by_rows else None, *cache, out, lse, self.workspace, stream)
 
     def check_status(self, stream=None) -> int:
         return swa_paged_check_status(self.params, self.workspace, stream)

@@ -157,7 +157,8 @@ struct Entry<int (*)(const P*, A...)> {
     X(swa_quantize_kv) \
     X(swa_paged_plan) \
     X(swa_paged_append) \
-    X(swa_paged_decode)
+    X(swa_paged_decode) \
+    X(swa_paged_decode_planned)
 
 #define SWA_DEFINE(name) \
     void* addr_##name = nullptr; \

@@ -38,8 +38,9 @@ int launch_paged_append(const swa_paged_params& p, const swa_rows& q, const swa_
                         const int32_t* slot, const float* inv_freq, const void* q_weight, const void* k_weight, void* q_out, void* k_pages,
                         void* v_pages, float* k_scale, float* v_scale, void* workspace, hipStream_t stream);
 
-int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_rows, const int32_t* row_start, const void* k_pages,
-                        const void* v_pages, const float* k_scale, const float* v_scale, const int32_t* block_table, const int32_t* cache_len,
-                        void* out, float* lse, void* workspace, hipStream_t stream);
+// (slot may be null)
+int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_rows, const int32_t* row_start, const int32_t* slot,
+                        const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale, const int32_t* block_table,
+                        const int32_t* cache_len, void* out, float* lse, void* workspace, hipStream_t stream);
 
 }  // namespace swa

@@ -44,6 +44,21 @@ static int check_pool(const swa_paged_params& p, const void* k_pages, const void
     return on16(k_pages) && on16(v_pages) && (!paged_int8(p) || (on16(k_scale) && on16(v_scale))) ? SWA_OK : SWA_ERR_ALIGNMENT;
 }
 
+static int decode_call(const swa_paged_params* params, const swa_rows& q, int32_t n_rows, const int32_t* row_start, const int32_t* slot,
+                       const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale, const int32_t* block_table,
+                       const int32_t* cache_len, void* out, float* lse, void* workspace, void* stream)
+{
+    int rc = validate_paged(params);
+    if (rc != SWA_OK) return rc;
+    if (!block_table || !cache_len || !out || !workspace) return SWA_ERR_NULL;
+    if ((rc = check_pool(*params, k_pages, v_pages, k_scale, v_scale)) != SWA_OK) return rc;
+    if ((rc = check_rows(*params, q, params->h_q)) != SWA_OK) return rc;
+    if (n_rows < 1 || n_rows > kMaxPlanRows || (!row_start && n_rows < params->b)) return SWA_ERR_BAD_SHAPE;
+    if (!on16(out) || !on16(workspace)) return SWA_ERR_ALIGNMENT;
+    return launch_paged_decode(*params, q, n_rows, row_start, slot, k_pages, v_pages, k_scale, v_scale, block_table, cache_len, out, lse,
+                               workspace, static_cast<hipStream_t>(stream));
+}
+
 __global__ void swa_paged_zero_kernel(int32_t* p)
 {
     if (threadIdx.x < 16) p[threadIdx.x] = 0;
@@ -124,15 +139,17 @@ int swa_paged_decode(const swa_paged_params* params, swa_rows q, int32_t n_rows,
                      const void* v_pages, const float* k_scale, const float* v_scale, const int32_t* block_table,
                      const int32_t* cache_len, void* out, float* lse, void* workspace, void* stream)
 {
-    int rc = swa::validate_paged(params);
-    if (rc != SWA_OK) return rc;
-    if (!block_table || !cache_len || !out || !workspace) return SWA_ERR_NULL;
-    if ((rc = swa::check_pool(*params, k_pages, v_pages, k_scale, v_scale)) != SWA_OK) return rc;
-    if ((rc = swa::check_rows(*params, q, params->h_q)) != SWA_OK) return rc;
-    if (n_rows < 1 || n_rows > swa::kMaxPlanRows || (!row_start && n_rows < params->b)) return SWA_ERR_BAD_SHAPE;
-    if (!swa::on16(out) || !swa::on16(workspace)) return SWA_ERR_ALIGNMENT;
-    return swa::launch_paged_decode(*params, q, n_rows, row_start, k_pages, v_pages, k_scale, v_scale, block_table, cache_len, out, lse,
-                                    workspace, static_cast<hipStream_t>(stream));
+    return swa::decode_call(params, q, n_rows, row_start, nullptr, k_pages, v_pages, k_scale, v_scale, block_table, cache_len, out, lse,
+                            workspace, stream);
+}
+
+int swa_paged_decode_planned(const swa_paged_params* params, swa_rows q, int32_t n_rows, const int32_t* row_start, const int32_t* slot,
+                             const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale,
+                             const int32_t* block_table, const int32_t* cache_len, void* out, float* lse, void* workspace, void* stream)
+{
+    if (!row_start || !slot) return SWA_ERR_NULL;
+    return swa::decode_call(params, q, n_rows, row_start, slot, k_pages, v_pages, k_scale, v_scale, block_table, cache_len, out, lse,
+                            workspace, stream);
 }
 
 }  // extern "C"

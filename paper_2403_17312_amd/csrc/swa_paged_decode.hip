@@ -27,7 +27,7 @@ namespace swa {
 struct PagedArgs {
     const char* q;
     int64_t q_stride;                              // bytes
-    const int32_t *row_start, *block_table, *cache_len;
+    const int32_t *row_start, *slot, *block_table, *cache_len;
     const char *k_pages, *v_pages;
     const float *k_scale, *v_scale;
     char* out;
@@ -156,6 +156,7 @@ __device__ __forceinline__ int paged_sequence(const PagedArgs& a, int s, int& ro
         if (row < a.row_start[s]) return 0;
     }
     if (n < 0 || row < 0 || row >= a.n_rows) return 0;
+    if (a.slot && a.slot[row] < 0) return 0;             // a row that the plan has not placed, whose query nobody wrote
     if (n > a.len_max) {
         too_long = true;
         return 0;
@@ -736,14 +737,15 @@ static void launch_paged_form(const PagedArgs& a, bool in_shares, hipStream_t st
                   stream, a, per);
 }
 
-int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_rows, const int32_t* row_start, const void* k_pages,
-                        const void* v_pages, const float* k_scale, const float* v_scale, const int32_t* block_table, const int32_t* cache_len,
-                        void* out, float* lse, void* workspace, hipStream_t stream)
+int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_rows, const int32_t* row_start, const int32_t* slot,
+                        const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale, const int32_t* block_table,
+                        const int32_t* cache_len, void* out, float* lse, void* workspace, hipStream_t stream)
 {
     PagedArgs a{};
     a.q = static_cast<const char*>(q.data);
     a.q_stride = q.stride * (p.dtype == SWA_F32 ? 4 : 2);
     a.row_start = row_start;
+    a.slot = slot;
     a.block_table = block_table;
     a.cache_len = cache_len;
     a.k_pages = static_cast<const char*>(k_pages);
