@@ -30,6 +30,9 @@ constexpr size_t kPagedPartialOffset = 256;    // the status word lies before th
 // Bytes of the partial results of swa_paged_decode, for any len_bound and window.
 size_t paged_partial_bytes(const swa_paged_params& p);
 
+// LDS of swa_paged_plan's workgroups, four lists of the same size.
+size_t paged_plan_lds(int32_t b);
+
 int launch_paged_plan(const swa_paged_params& p, const int32_t* new_cnt, const int32_t* cache_len, int32_t* new_len, int32_t* block_table,
                       int32_t* free_ring, const int32_t* free_state, int32_t* free_state_out, int32_t max_rows, int32_t* row_start,
                       int32_t* slot, int32_t* pos, void* workspace, hipStream_t stream);

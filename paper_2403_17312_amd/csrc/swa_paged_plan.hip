@@ -61,12 +61,18 @@ __device__ __forceinline__ int above(const int32_t* sums, int n, int32_t x)
     return lo;
 }
 
+// Sequences that each of the four lists in LDS has room for: even, so that the sums of the waves, pairs of numbers at the fourth one's beginning, lie on
+// 8 bytes; and enough for those of sixteen waves.
+__host__ __device__ constexpr int plan_room(int b) { return ((b < 32 ? 32 : b) + 1) & ~1; }
+
+size_t paged_plan_lds(int32_t b) { return 4 * sizeof(int32_t) * (size_t)plan_room(b); }
+
 // PER: sequences of a thread while the sums are formed.
 template <int THREADS, int PER>
 __global__ void __launch_bounds__(THREADS) swa_paged_plan_kernel(PlanArgs a)
 {
-    extern __shared__ int32_t lds[];
-    const int tid = threadIdx.x, b = a.b, ps = a.page_size, room = b < 32 ? 32 : b;
+    extern __shared__ __align__(16) int32_t lds[];
+    const int tid = threadIdx.x, b = a.b, ps = a.page_size, room = plan_room(b);
     int32_t* const rows_to = lds;                  // rows up to and with sequence s
     int32_t* const asked_to = lds + room;          // pages that sequences up to s ask for
     int32_t* const back_to = lds + 2 * room;       // pages that sequences up to s give back
@@ -77,7 +83,7 @@ __global__ void __launch_bounds__(THREADS) swa_paged_plan_kernel(PlanArgs a)
     int32_t head = a.free_state[0], free = a.free_state[1];
     int32_t bits = 0;
     auto pages_of = [&](int32_t t) { return t > 0 ? (int32_t)(((uint64_t)(uint32_t)(t - 1) * a.page_mul) >> a.page_shift) + 1 : 0; };
-    auto in_ring = [&](int32_t i) {                // place i behind the head, 0 <= i < n_pages + n_pages
+    auto in_ring = [&](int32_t i) {                // place i behind the head, 0 <= i <= n_pages
         const uint32_t at = (uint32_t)head + (uint32_t)i;
         return (int32_t)(at < (uint32_t)a.n_pages ? at : at - (uint32_t)a.n_pages);
     };
@@ -211,8 +217,8 @@ int launch_paged_plan(const swa_paged_params& p, const int32_t* new_cnt, const i
                paged_status(workspace), p.b, p.page_size, p.n_pages, p.max_pages, max_rows, 0, 0};
     page_divisor(p.page_size, a.page_mul, a.page_shift);
     const int64_t items = max_rows > p.b ? max_rows : p.b;
-    const size_t lds = 4 * sizeof(int32_t) * (size_t)(p.b < 32 ? 32 : p.b);
-    static_assert(4 * sizeof(int32_t) * SWA_MAX_PAGED_SEQS <= 64 * 1024 && SWA_MAX_PAGED_SEQS <= 4 * 1024, "a workgroup holds all sums");
+    const size_t lds = paged_plan_lds(p.b);
+    static_assert(4 * sizeof(int32_t) * plan_room(SWA_MAX_PAGED_SEQS) <= 64 * 1024 && SWA_MAX_PAGED_SEQS <= 4 * 1024, "a workgroup holds all sums");
     // 1024 sequences with 256 / 512 / 1024 threads in a workgroup 8.5 / 7.3 / 8.1 us; 4096 with 256 / 1024 15.9 / 10.4; 1 and 256 sequences 3.7 and 4.9,
     // a launch that does nothing 3.5
     auto launch = [&](auto kernel, int threads) {
