@@ -208,7 +208,10 @@ __global__ void __launch_bounds__(kAppendThreads) swa_paged_append_kernel(Append
                 float square = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) square = __builtin_fmaf(x[i], x[i], square);
-                norm = __builtin_amdgcn_rsqf(group_sum<kLanes>(square) * (1.f / D) + a.eps);
+                const float mean = group_sum<kLanes>(square) * (1.f / D) + a.eps;
+                // (the root's instruction takes what lies below fp32's normal numbers for 0, and without an eps such a row would be infinite)
+                const int up = mean < 0x1p-100f ? 32 : 0;
+                norm = __builtin_amdgcn_ldexpf(__builtin_amdgcn_rsqf(__builtin_amdgcn_ldexpf(mean, 2 * up)), up);
             }
             float y[8], z[8];
             if (!NEIGHBOURS) raw.from_lane(mine * kLanes + other).widen(y);
