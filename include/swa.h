@@ -510,7 +510,8 @@ int swa_paged_check_status(const swa_paged_params *params, void *workspace, void
  *      the next call), new_len[s] = 0.
  * A page belongs to one sequence: a page that two rows of the table name is handed back by both.
  * A cache_len above max_pages * page_size, and a page number outside the pool in the ring or in a finished sequence's row, set
- * the SWA_ERR_BAD_REQUEST bit; such a sequence is left alone, such a page gets slot -1.
+ * the SWA_ERR_BAD_REQUEST bit; such a sequence is left alone, such a page gets slot -1.  So does a free_state outside the ring (head
+ * in 0..n_pages-1, count in 0..n_pages), which counts as an empty one.
  *   new_cnt, cache_len [b] (in); new_len [b], row_start [b+1], slot, pos [max_rows], free_state_out [2] (out);
  *   block_table, free_ring [n_pages] (in/out); free_state [2] (in); 1 <= max_rows <= 2^24.
  */

@@ -95,8 +95,10 @@ __global__ void __launch_bounds__(THREADS) swa_paged_plan_kernel(PlanArgs a)
         count[i] = s0 + i < b ? a.new_cnt[s0 + i] : 0;
         len[i] = s0 + i < b ? a.cache_len[s0 + i] : -1;
     }
-    free = free < 0 ? 0 : (free > a.n_pages ? a.n_pages : free);
-    head = (head < 0 || head >= a.n_pages) ? 0 : head;
+    if ((uint32_t)free > (uint32_t)a.n_pages || (uint32_t)head >= (uint32_t)a.n_pages) {   // no ring's: whatever lay there may be in use
+        head = free = 0;
+        bits |= kStatusBadRequestBit;
+    }
 #pragma unroll
     for (int i = 0; i < PER; ++i) sum = add_saturating(sum, count[i] < 0 ? 0 : (count[i] > kRowsSaturate ? kRowsSaturate : count[i]));
     int32_t rows = sums_before(sum, 0, wave_sums).x;
