@@ -553,6 +553,9 @@ int swa_paged_append(const swa_paged_params *params, swa_rows q, swa_rows k, swa
  * there, which swa_paged_append has not written.  swa_paged_decode_planned leaves such sequences out.
  * A sequence longer than max_pages * page_size or a stated len_bound is skipped, and the SWA_ERR_CAPACITY bit is set.  Tokens of
  * pages outside the pool are left out of the sums, and the SWA_ERR_BAD_REQUEST bit is set.
+ * SWA_ERR_CAPACITY also for more than a launch holds: with b * h_kv times the groups of 16 (above 16 heads to a key head: 32) query heads of a
+ * key head, and n the tokens that a sequence may see (of its table, len_bound, window), 2^24 of them where n is 257 to 1023,
+ * 2^26 where it is less; and b * h_kv * n / 128 of 2^31.
  *   q [n_rows, h_q, d] (in); row_start [b+1] or NULL (then n_rows >= b); out [n_rows, h_q, d] dense, lse [n_rows, h_q] float32 or
  *   NULL (out).
  */

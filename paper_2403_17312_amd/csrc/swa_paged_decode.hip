@@ -712,7 +712,7 @@ __global__ void __launch_bounds__(256) swa_paged_join_shares_kernel(PagedArgs a,
 }
 
 template <typename T, typename C, int D>
-static void launch_paged_form(const PagedArgs& a, bool in_shares, hipStream_t stream)
+static int launch_paged_form(const PagedArgs& a, bool in_shares, hipStream_t stream)
 {
     const int64_t units = (int64_t)a.b * a.h_kv, works = (in_shares ? a.ranges : units * a.ranges);
     const dim3 grid((unsigned)((works + 7) / 8 * 8 * a.row_tiles));
@@ -725,16 +725,18 @@ static void launch_paged_form(const PagedArgs& a, bool in_shares, hipStream_t st
     auto kernel = in_shares ? (one ? swa_paged_decode_kernel<T, C, D, true, 1, 4> : swa_paged_decode_kernel<T, C, D, true, 2, 4>)
                   : single  ? (one ? swa_paged_decode_kernel<T, C, D, false, 1, 1> : swa_paged_decode_kernel<T, C, D, false, 2, 1>)
                             : (one ? swa_paged_decode_kernel<T, C, D, false, 1, 4> : swa_paged_decode_kernel<T, C, D, false, 2, 4>);
+    if (grid.x * UINT64_C(64) * (single ? 1 : kPagedWaves) > 0xffffffffULL) return SWA_ERR_CAPACITY;    // (threads of a launch; the join's are fewer)
     launch_kernel(kernel, grid, dim3(single ? 64 : 64 * kPagedWaves), in_shares ? sizeof(int) * ((size_t)a.b + 1) : 0, stream, a);
-    if (a.ranges == 1) return;
+    if (a.ranges == 1) return SWA_OK;
     if (!in_shares) {
         launch_kernel(swa_paged_join_chunks_kernel<T, D>, dim3((unsigned)((int64_t)a.b * a.h_q)), dim3(256), 0, stream, a);
-        return;
+        return SWA_OK;
     }
     int per = 1;                                         // (where a sequence has few pieces, a workgroup joins several heads)
     while (per < 1024 / D && per < a.heads && a.ranges < 4 * units * per) per *= 2;
     launch_kernel(swa_paged_join_shares_kernel<T, D>, dim3((unsigned)((int64_t)a.ranges * a.row_tiles * ((a.heads + per - 1) / per))), dim3(256), 0,
                   stream, a, per);
+    return SWA_OK;
 }
 
 int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_rows, const int32_t* row_start, const int32_t* slot,
@@ -806,10 +808,11 @@ int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_
     a.begun = reinterpret_cast<int4*>(a.part_sum + paged_piece_rows(p) * 2);
 
 #define SWA_PAGED(T, C) (p.d == 64 ? launch_paged_form<T, C, 64>(a, in_shares, stream) : launch_paged_form<T, C, 128>(a, in_shares, stream))
-    if (p.dtype == SWA_F32) SWA_PAGED(F32, F32);
-    else if (p.dtype == SWA_F16) paged_int8(p) ? SWA_PAGED(F16, Q8) : SWA_PAGED(F16, F16);
-    else paged_int8(p) ? SWA_PAGED(BF16, Q8) : SWA_PAGED(BF16, BF16);
+    const int rc = p.dtype == SWA_F32   ? SWA_PAGED(F32, F32)
+                   : p.dtype == SWA_F16 ? (paged_int8(p) ? SWA_PAGED(F16, Q8) : SWA_PAGED(F16, F16))
+                                        : (paged_int8(p) ? SWA_PAGED(BF16, Q8) : SWA_PAGED(BF16, BF16));
 #undef SWA_PAGED
+    if (rc != SWA_OK) return rc;
     return hipGetLastError() == hipSuccess ? SWA_OK : SWA_ERR_HIP;
 }
 
