@@ -37,6 +37,9 @@ int launch_paged_plan(const swa_paged_params& p, const int32_t* new_cnt, const i
                       int32_t* free_ring, const int32_t* free_state, int32_t* free_state_out, int32_t max_rows, int32_t* row_start,
                       int32_t* slot, int32_t* pos, void* workspace, hipStream_t stream);
 
+// Waves that share a row of swa_paged_append, as a power of two; wide: in fp32.
+int paged_append_log_parts(bool wide, bool codes, int passes, int64_t n_rows);
+
 int launch_paged_append(const swa_paged_params& p, const swa_rows& q, const swa_rows& k, const swa_rows& v, int32_t n_rows, const int32_t* pos,
                         const int32_t* slot, const float* inv_freq, const void* q_weight, const void* k_weight, void* q_out, void* k_pages,
                         void* v_pages, float* k_scale, float* v_scale, void* workspace, hipStream_t stream);

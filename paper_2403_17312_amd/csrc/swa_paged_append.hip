@@ -260,6 +260,28 @@ static void launch_append_form(const AppendArgs& a, bool neighbours, bool past, 
     launch_kernel(kernel, grid, dim3(kAppendThreads), 0, stream, a);
 }
 
+// Waves that share a row's passes, as a power of two.  A wave has one pass's loads under way, so that few waves do not fill the chip; but each begins with the
+// angles of the row, which its passes have to outweigh.  So they are halved below a number of waves that grows with the passes left to each.
+// us with 1 / 2 / 4 / 8 waves a row: 32 query and 8 key heads of 128 bf16 channels (12 passes), 400 rows 10.0 / 7.1 / 5.9 / 7.1, 512 10.4 / 7.5 / 6.5 / 7.5, 1024 11.2 / 8.9 / 8.9, 2048 12.9 /
+// 12.2, 3000 15.4 / 16.4; 28 and 4 heads (9 passes), 400 8.6 / 6.5 / 5.5 / 5.9, 2048 11.1 / 10.3, 3000 12.8 / 13.6; 64 and 8 heads (20 passes), 1024 15.7 / 11.6 / 11.1,
+// 1800 17.9 / 15.8, 5000 45.0 / 50.0.  fp32 has twice the bytes under way: 12 passes, 900 12.9 / 11.1 / 12.0, 1800 19.6 / 19.4.
+// Beyond that the chip is full, and what counts is how full the last waves leave it, whose time is that of a row.  Where rows are long and those waves are a third of
+// it or less, two waves a row end sooner (of four rounds a few per cent at most: then no more): codes (7168 waves at once) of 20 passes, 7000 rows 61.7 / 62.5, 7300 73.7 / 69.5, 8100 80.2 / 73.9, 9000 84.7 / 79.4, 12000
+// 102.7 / 102.4, 14500 127.1 / 122.0; 16 bits (8192), 16 passes, 8100 59.3 / 59.0, 8400 69.1 / 64.9, 9000 73.3 / 68.3, 12000 84.6 / 84.4; of 12 passes 10000 rows 58.9 / 56.9,
+// but 16000 83.4 / 85.3 as codes.  Long rows in fp32 gain at any count: 20 passes, 3000 rows 58.2 / 57.5, 6000 115 / 109, 8000 155 / 142.
+int paged_append_log_parts(bool wide, bool codes, int passes, int64_t n_rows)
+{
+    const int64_t at_once = wide || codes ? 7168 : 8192;     // by the kernels' registers
+    auto more = [&](int64_t waves, int each) {
+        const int64_t few = 1024 + (wide ? 64 : 128) * (int64_t)each, last = waves % at_once;
+        if (waves < (few < at_once / 2 ? few : at_once / 2)) return true;
+        return each >= 16 && waves <= 4 * at_once && (wide || (waves > at_once && last > 0 && last <= at_once / 3));
+    };
+    int log_parts = 0;
+    while ((1 << log_parts) < passes && more(n_rows << log_parts, passes >> log_parts)) ++log_parts;
+    return log_parts;
+}
+
 int launch_paged_append(const swa_paged_params& p, const swa_rows& q, const swa_rows& k, const swa_rows& v, int32_t n_rows, const int32_t* pos,
                         const int32_t* slot, const float* inv_freq, const void* q_weight, const void* k_weight, void* q_out, void* k_pages,
                         void* v_pages, float* k_scale, float* v_scale, void* workspace, hipStream_t stream)
@@ -295,12 +317,8 @@ int launch_paged_append(const swa_paged_params& p, const swa_rows& q, const swa_
         a.axis_end[i] = i + 1 < p.axes ? end : INT32_MAX;
     }
     a.eps = p.eps;
-    // A row's passes are shared out among waves until there are 2048, and further while they are many: us with 1 / 2 / 4 / 8 waves a row, 32 query and 8 key
-    // heads of 128 bf16 channels (12 passes): 512 rows - / - / 7.0 / 7.8, 1024 - / 8.9 / 8.9 / 11.1, 2048 13.1 / 12.3 / 13.0 / -, 4096 19.3 / 21.0; 64 and 8 heads, fp16
-    // into codes (20 passes), 8192 rows 92 / 82.
     const int of_wave = 64 / (p.d / 8), passes = (p.h_q + of_wave - 1) / of_wave + 2 * ((p.h_kv + of_wave - 1) / of_wave);
-    auto more = [&](int64_t waves, int each) { return waves < 2048 || (waves <= 2048 && each >= 12) || (waves <= 8192 && each >= 16); };
-    while ((1 << a.log_parts) < passes && more((int64_t)n_rows << a.log_parts, passes >> a.log_parts)) ++a.log_parts;
+    a.log_parts = paged_append_log_parts(p.dtype == SWA_F32, paged_int8(p), passes, n_rows);
     // Many rows fill the caches with what nothing reads soon: 4096 rows as above 26.6 us stored through them, 19.3 past them; 8192 rows 49.5, 44.5 (4.5
     // TB/s); 256 rows and the attention behind them 47.1, 45.7.  Of few, the attention finds queries and keys there: 1 row and 100 tokens 8.7, 9.0.
     const bool past = (int64_t)n_rows * (p.h_q + 2 * p.h_kv) * p.d * bytes >= (2 << 20);
