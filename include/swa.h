@@ -546,8 +546,8 @@ int swa_paged_append(const swa_paged_params *params, swa_rows q, swa_rows k, swa
  * swa_paged_plan writes it) the last of rows row_start[s] .. row_start[s+1] - 1.  Sequences with a negative cache_len, without
  * rows, or with a row beyond n_rows are skipped: nothing is written for them.  Where no token is left or every logit is -inf (so
  * for cache_len = 0), out = 0 and lse = -inf.
- * Accumulated in fp32; the weights are rounded to dtype (8-bit codes: to 16 bits of mantissa) for their product with the
- * values (relative to themselves; in fp16 those below 2^-29 of the largest lose bits, those below 2^-40 count nothing), out is rounded once.  A call's results do not depend on the order in which its workgroups run; a sequence's may differ
+ * Accumulated in fp32; for their product with the values the weights are rounded to 15 bits in bf16, 21 in fp16 (2^-39 of the largest at the
+ * least), 16 over 8-bit codes; out is rounded once.  A call's results do not depend on the order in which its workgroups run; a sequence's may differ
  * in their last bits with the call's other lengths and with len_bound, which say where its tokens are cut into pieces.
  * A sequence that the plan refused keeps its rows in row_start and its cache_len: this call attends for it with whatever q holds
  * there, which swa_paged_append has not written.  swa_paged_decode_planned leaves such sequences out.

@@ -136,6 +136,33 @@ __device__ __forceinline__ uint32_t round2(float lo, float hi)
     else return f32x2_to_bf16x2_bits(lo, hi);
 }
 
+// Eight weights (0 or more) as two numbers of the matrix cores' type each, big and rest.
+//   CODES: rounded to the nearest both times.
+//   else: the values may be infinite, and a weight's two numbers have to be 0 or of its sign for an infinity to stay one.  So big is cut off, from what lies just below the
+//   weight (bf16), or rest is raised to fp16's smallest number (2^-39 of the largest weight; not for a weight of 0).
+template <typename P, bool CODES>
+__device__ __forceinline__ void split8(const float* w, Vec16& big, Vec16& rest)
+{
+    float f[8], r[8];
+    if constexpr (CODES) {
+        big = Vec16{round2<P>(w[0], w[1]), round2<P>(w[2], w[3]), round2<P>(w[4], w[5]), round2<P>(w[6], w[7])};
+    } else if constexpr (std::is_same_v<P, F16>) {
+        auto cut = [&](int i) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(w[i], w[i + 1])); };
+        big = Vec16{cut(0), cut(2), cut(4), cut(6)};
+    } else {
+        auto below = [&](int i) { return __builtin_elementwise_sub_sat(f2u(w[i]), 1u); };
+        auto cut = [&](int i) { return __builtin_amdgcn_perm(below(i + 1), below(i), 0x07060302u); };
+        big = Vec16{cut(0), cut(2), cut(4), cut(6)};
+    }
+    unpack<P>(big, f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        r[i] = w[i] - f[i];
+        if constexpr (!CODES && std::is_same_v<P, F16>) r[i] = fmaxf(r[i], fminf(w[i], 0x1p-24f));
+    }
+    rest = Vec16{round2<P>(r[0], r[1]), round2<P>(r[2], r[3]), round2<P>(r[4], r[5]), round2<P>(r[6], r[7])};
+}
+
 template <typename V>
 __device__ __forceinline__ V load_values(const char* p)
 {
@@ -205,12 +232,13 @@ __global__ void __launch_bounds__(64 * WAVES, paged_two(Elem<C>::kBytes * D, ROW
 {
     constexpr bool kCodes = std::is_same_v<C, Q8>, kWide = std::is_same_v<C, F32>;
     // Codes are exact in either 16-bit type.  Keys get the queries' type; values get bf16, whose range the weights need, which are products with a
-    // scale there, and the weights go as two bf16 numbers, which hold 16 bits.
+    // scale there.  In 16 bits weights go as two numbers, which hold 15 or 16 bits in bf16 and 21 in fp16: one alone left the output a tenth to a quarter farther from
+    // the exact one than its own rounding does, and the second product is free (decode of 128 ragged sequences, bf16, 353.7 / 353.0 us, of one of 131071 tokens, fp16, 51.6 / 51.8).
     constexpr int kTiles = kWide && (D == 128 || ROWS == 2) ? 1 : 2, kKeys = 16 * kTiles, kRow = D * Elem<C>::kBytes;
     constexpr int kSteps = kWide ? D / 16 : D / 32;      // operands of a logit
     constexpr int kChannels = D / 16;                    // of V in a lane
-    // A weight is exp2(x - top + kRaise).  fp16 has 2^-14 to 2^15 for normal numbers: raised so far the largest weight is 2^15, and one keeps its bits down to
-    // 2^-29 of it and is lost below 2^-40.  Without, a wave lost what lies 17.4 nats below its loudest token, which for 131072 such tokens beside one
+    // A weight is exp2(x - top + kRaise).  fp16 has 2^-14 to 2^15 for normal numbers: raised so far the largest weight is 2^15 and half a step of
+    // the smallest numbers 2^-40 of it.  Without, a wave lost what lies 17.4 nats below its loudest token, which for 131072 such tokens beside one
     // of small value was 6.7 % of the output.  The sum carries the same factor, so nothing takes it back but the maximum, as it is handed on.
     constexpr float kRaise = std::is_same_v<C, F16> ? 15.f : 0.f;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, j = lane >> 4;
@@ -488,16 +516,7 @@ __global__ void __launch_bounds__(64 * WAVES, paged_two(Elem<C>::kBytes * D, ROW
                     typedef std::conditional_t<kCodes, BF16, T> P;
                     Vec16 p[ROWS], p_rest[ROWS];
 #pragma unroll
-                    for (int g = 0; g < ROWS; ++g) {
-                        const float* const w = x[g][u];
-                        p[g] = Vec16{round2<P>(w[0], w[1]), round2<P>(w[2], w[3]), round2<P>(w[4], w[5]), round2<P>(w[6], w[7])};
-                        if constexpr (kCodes) {
-                            float f[8];
-                            unpack<BF16>(p[g], f);
-                            p_rest[g] = Vec16{round2<BF16>(w[0] - f[0], w[1] - f[1]), round2<BF16>(w[2] - f[2], w[3] - f[3]),
-                                              round2<BF16>(w[4] - f[4], w[5] - f[5]), round2<BF16>(w[6] - f[6], w[7] - f[7])};
-                        }
-                    }
+                    for (int g = 0; g < ROWS; ++g) split8<P, kCodes>(x[g][u], p[g], p_rest[g]);
 #pragma unroll
                     for (int e = 0; e < kChannels; ++e) {
                         Vec16 op;
@@ -515,7 +534,7 @@ __global__ void __launch_bounds__(64 * WAVES, paged_two(Elem<C>::kBytes * D, ROW
 #pragma unroll
                         for (int g = 0; g < ROWS; ++g) {
                             acc[g][e] = mfma16<P>(op, p[g], acc[g][e]);
-                            if constexpr (kCodes) acc[g][e] = mfma16<BF16>(op, p_rest[g], acc[g][e]);
+                            acc[g][e] = mfma16<P>(op, p_rest[g], acc[g][e]);
                         }
                     }
                 }
