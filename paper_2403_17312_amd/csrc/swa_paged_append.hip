@@ -6,8 +6,8 @@
 // neighbouring pairs, in the same lane).  A wave takes one row's queries, keys and values in turn, a wave's heads of one kind at a time, with the
 // next ones' loads under way.  The angles depend on row and channel alone: a lane forms its own sines and cosines once for all
 // heads of the row, and with the norm's weights makes two factors of them, y = (x_i a_i + x_j b_i) / rms.  An angle of a far position has no
-// digits left in fp32 (position 10^6: 0.06), so position * inv_freq / 2 pi is an fp64 product, whose whole turns go before it is rounded;
-// the hardware's sine and cosine of a turn are within 2^-22.9 (all of [-1/2, 1/2], in steps of 2^-24).
+// digits left in fp32 (position 10^6: 0.06), so position * inv_freq / 2 pi is an fp64 product, whose whole turns go before it is rounded.  In 16 bits
+// the hardware's sine and cosine of that serve, within 2^-22.9 (all of [-1/2, 1/2], in steps of 2^-24); fp32 rows get better ones.
 #include <type_traits>
 
 #include "swa_paged.hpp"
@@ -92,6 +92,28 @@ __device__ __forceinline__ uint32_t group_max_bits(uint32_t v)
     return v;
 }
 
+// Sine and cosine of an angle in turns.  WIDE: of x quarter turns from the nearest whole one, |x| <= 1/2, by their Taylor series (the first terms left out are below 2^-29 and
+// 2^-33).  The hardware's left rotated fp32 rows 1.66 times as far (rms) from the exact ones as sines rounded once do, these 1.11 times: 11.03 -> 11.19 us for 1001 rows of 96 heads.
+template <bool WIDE>
+__device__ __forceinline__ void sine_cosine(double turn, float& sine, float& cosine)
+{
+    if constexpr (WIDE) {
+        const double quarters = 4.0 * (turn - __builtin_rint(turn)), whole = __builtin_rint(quarters);
+        const float x = (float)(quarters - whole), y = x * x;
+        const int at = (int)whole;                   // -2 .. 2
+        const float s = x * __builtin_fmaf(y, __builtin_fmaf(y, __builtin_fmaf(y, __builtin_fmaf(y, 1.6044118e-4f, -4.6817541e-3f), 7.9692626e-2f), -0.64596410f), 1.5707963f);
+        const float c = __builtin_fmaf(y, __builtin_fmaf(y, __builtin_fmaf(y, __builtin_fmaf(y, __builtin_fmaf(y, -2.5202042e-5f, 9.1926027e-4f), -2.0863481e-2f), 0.25366951f), -1.2337006f), 1.f);
+        sine = at & 1 ? c : s;
+        cosine = at & 1 ? s : c;
+        sine = at & 2 ? -sine : sine;
+        cosine = (at + 1) & 2 ? -cosine : cosine;
+    } else {
+        const float rest = (float)(turn - __builtin_rint(turn));
+        sine = __builtin_amdgcn_sinf(rest);
+        cosine = __builtin_amdgcn_cosf(rest);
+    }
+}
+
 // A lane's channels of the heads of one pass.
 template <typename T, int D>
 __device__ __forceinline__ void fetch_heads(Raw8<T>& raw, const AppendArgs& a, int row, int pass, int q_passes, int kv_passes, int mine, int sub)
@@ -157,10 +179,7 @@ __global__ void __launch_bounds__(kAppendThreads) swa_paged_append_kernel(Append
             int axis = 0;
 #pragma unroll
             for (int x = 0; x + 1 < SWA_MAX_ROPE_AXES; ++x) axis += pair >= a.axis_end[x];
-            const double turn = (double)a.pos[(int64_t)axis * a.n_rows + row] * (double)a.inv_freq[pair] * 0.15915494309189533577;
-            const float rest = (float)(turn - __builtin_rint(turn));
-            s[i] = __builtin_amdgcn_sinf(rest);
-            c[i] = __builtin_amdgcn_cosf(rest);
+            sine_cosine<std::is_same_v<T, F32>>((double)a.pos[(int64_t)axis * a.n_rows + row] * (double)a.inv_freq[pair] * 0.15915494309189533577, s[i], c[i]);
             if (NEIGHBOURS || sub < half) s[i] = -s[i];
         }
     }
