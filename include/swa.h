@@ -526,8 +526,9 @@ int swa_paged_plan(const swa_paged_params *params, const int32_t *new_cnt, const
  *   rotation  (x_i, x_j) <- (x_i cos a - x_j sin a, x_j cos a + x_i sin a) for the pairs of the first rot_dim channels, with the
  *             angle a = pos[axis of the pair][r] * inv_freq[pair]    (queries and keys)
  * q_out gets the queries, slot[r] of k_pages and v_pages the keys and the values as they came.  All in fp32, the angle in
- * fp64 until it is reduced to one turn (its sine and cosine to 2^-22.9 where dtype has 16 bits); rounded once.  With SWA_KV_INT8 a row is stored as scale = max |x| / 127 and codes
- * round(x / scale), ties to even (zeros where scale is below 2^-126); a row with a value that is not finite reads back as NaN.
+ * fp64 until it is reduced to one turn (its sine and cosine to 2^-22.9 where dtype has 16 bits); rounded once.  With SWA_KV_INT8
+ * a row is stored as scale = max |x| / 127 and codes round(x / scale), fp32 divisions rounded correctly, ties to even (zeros where
+ * scale is below 2^-126); a row with a value that is not finite reads back as NaN.
  * A row with a negative slot is left out: nothing is written for it.  A slot outside the pool is left out too and
  * sets the SWA_ERR_BAD_REQUEST bit.  The slots of one call are distinct (as swa_paged_plan makes them): of two rows with the
  * same slot either may end up in it, or some heads of each.

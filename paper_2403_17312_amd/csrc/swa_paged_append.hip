@@ -114,6 +114,15 @@ __device__ __forceinline__ void sine_cosine(double turn, float& sine, float& cos
     }
 }
 
+// x / by rounded correctly, from by's reciprocal: a product, and two steps that take the remainder, exact in an FMA, into account (the first makes the quotient one of the two
+// neighbours, the second the nearer one).  A product alone gave another code where a quotient lies half way between two.
+__device__ __forceinline__ float quotient(float x, float by, float inverse)
+{
+    float q = x * inverse;
+    q = __builtin_fmaf(__builtin_fmaf(-q, by, x), inverse, q);
+    return __builtin_fmaf(__builtin_fmaf(-q, by, x), inverse, q);
+}
+
 // A lane's channels of the heads of one pass.
 template <typename T, int D>
 __device__ __forceinline__ void fetch_heads(Raw8<T>& raw, const AppendArgs& a, int row, int pass, int q_passes, int kv_passes, int mine, int sub)
@@ -255,13 +264,14 @@ __global__ void __launch_bounds__(kAppendThreads) swa_paged_append_kernel(Append
         }
         // (rows below 2^-119 have no scale with a reciprocal in fp32: their codes are 0)
         top = group_max_bits<kLanes>(top);
-        const float scale = u2f(top < 0x7f800000u ? top : 0x7fc00000u) * (1.f / 127.f);
+        const float scale = quotient(u2f(top < 0x7f800000u ? top : 0x7fc00000u), 127.f, 1.f / 127.f);
         const bool tiny = scale < 1.17549435e-38f;
-        const float inverse = tiny ? 0.f : __builtin_amdgcn_rcpf(scale);
+        float inverse = __builtin_amdgcn_rcpf(scale);
+        inverse = tiny ? 0.f : __builtin_fmaf(__builtin_fmaf(-scale, inverse, 1.f), inverse, inverse);
         uint32_t codes[2] = {0u, 0u};
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float t = fminf(fmaxf(rintf(x[i] * inverse), -127.f), 127.f);
+            const float t = fminf(fmaxf(rintf(quotient(x[i], scale, inverse)), -127.f), 127.f);
             codes[i / 4] |= ((uint32_t)(int32_t)t & 0xffu) << (8 * (i % 4));
         }
         if (there) {
