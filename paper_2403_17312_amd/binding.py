@@ -487,7 +487,8 @@ def swa_paged_decode_planned(params: SwaPagedParams, q, n_rows: int, row_start, 
 
 class PagedCache:
     """Device tensors of a paged cache: one pool per layer, one plan for all of them (allocation plumbing, and checks of what is
-    handed in).  A step is plan(), then append() and decode() for every layer."""
+    handed in).  A step is plan(), then append() and decode() for every layer.  plan() swaps the two copies of the lengths and of the ring's
+    state, so a captured step replays with the copies that it was captured with: capture two steps and replay them in turn."""
 
     def __init__(self, params: SwaPagedParams, layers: int = 1, device="cuda"):
         p = self.params = params
@@ -518,7 +519,7 @@ class PagedCache:
 
     def plan(self, new_cnt, slot, pos, stream=None) -> None:
         """new_cnt [b] (-1: finished); slot and pos [rows] are filled.  cache_len counts the new tokens afterwards.  A sequence for which pages or
-        rows ran out is refused: its rows have slots of -1, its cache_len stays."""
+        rows ran out is refused: its rows have slots of -1, its cache_len stays.  slot and pos have a row at least, also where none is new."""
         self._expect("new_cnt", new_cnt, (self.params.b,), torch.int32)
         self._expect("slot", slot, (slot.numel(),), torch.int32)
         self._expect("pos", pos, slot.shape, torch.int32)

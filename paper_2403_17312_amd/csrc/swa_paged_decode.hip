@@ -9,8 +9,8 @@
 //            holds whole sequences and at most two pieces.  128 sequences of 512 to 8192 tokens, 8 key heads of 128 bf16 channels: chunks
 //            425 us, shares 353 (6.5 TB/s).
 // Pieces leave partial results, which a second, small launch joins in their order.
-// All products go to the matrix cores, whose 16 columns are the query heads: also a single head's, since the matrix cores have
-// fifteen times the time that HBM leaves them.
+// All products go to the matrix cores, whose 16 columns are the query heads: also a single head's, since at their peak they are done in a fifteenth of the
+// time that HBM takes for 16 bits, a seventh for codes, and in fp32 something more than a third (with 32 columns: twice those parts).
 //   logits   S^T = K Q^T: a lane's operand is 16 bytes of one key, as it lies in memory; a 64-byte piece of 16 keys a load.
 //   values   O^T = V^T P^T: S^T leaves lane (j, c) with keys 4j..4j+3 of column c, which is what the product with V takes from that lane
 //            if its contraction runs over the keys in that order; nothing moves between lanes.  For V^T a lane loads the same D / 16
@@ -243,7 +243,9 @@ __global__ void __launch_bounds__(64 * WAVES, paged_two(Elem<C>::kBytes * D, ROW
     constexpr float kRaise = std::is_same_v<C, F16> ? 15.f : 0.f;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, j = lane >> 4;
 
-    // Row tiles of one range read the same pages: eight ranges, then the same ones' next row tile, so that they meet in one XCD's L2.
+    // Row tiles of one range read the same pages: eight ranges, then the same ones' next row tile, so that they meet in one XCD's L2.  Reads of HBM per
+    // launch against the pages: 71 heads on one key head (three tiles), 16 sequences of 1000 to 8000 tokens, 64 channels, 1.02 times; 128 heads (four), 64 of 8000, 128
+    // channels, 2.3 times.
     const int eighth = blockIdx.x >> 3, work = (eighth / a.row_tiles) * 8 + (blockIdx.x & 7), tile = eighth % a.row_tiles;
     const int heads = a.group - 16 * ROWS * tile < 16 * ROWS ? a.group - 16 * ROWS * tile : 16 * ROWS;
 
