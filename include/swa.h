@@ -575,6 +575,76 @@ int swa_paged_decode_planned(const swa_paged_params *params, swa_rows q, int32_t
                              const int32_t *block_table, const int32_t *cache_len, void *out, float *lse, void *workspace, void *stream);
 
 /*
+ * Sparse attention over pages: swa_paged_bounds keeps the smallest and the largest key of every page, channel by channel, as the pages fill;
+ * swa_paged_score bounds the logits of a page's keys by them; swa_paged_select takes the pages of highest score for each sequence and key head;
+ * swa_paged_decode_selected attends over the tokens of those.  A step is swa_paged_append, bounds, score, select, decode (once a layer).  The
+ * selection is by pages, so page_size says how fine it is, and a score reads 2 / page_size of what the keys of all tokens would take.  params->window is
+ * 0 for score, select and decode (SWA_ERR_BAD_SHAPE).  Where a call takes row_start and slot, they say whose rows q holds as in swa_paged_decode (row_start, slot NULL:
+ * row s is sequence s) and swa_paged_decode_planned (sequences whose row has a negative slot are left out, too); slot without row_start is SWA_ERR_NULL.
+ *
+ * swa_paged_bounds: for every row r < n_rows with slot[r] >= 0, after swa_paged_append has written it:
+ *   bounds[page][head][0][c] = min, [1][c] = max of K[c] over the page's tokens, of those that it had and the call's; a page whose first token
+ *   (offset 0) is among the call's begins anew.  Values are the cache's (with SWA_KV_INT8 code times scale in fp32, rounded to dtype); what is no number stays
+ *   in them.  The rows of one page follow each other in `slot` (as swa_paged_plan makes them).  The same call again gives the same bounds.
+ *   A slot outside the pool is left out and sets the SWA_ERR_BAD_REQUEST bit.
+ *   slot [n_rows], k_pages, k_scale (in); bounds [n_pages, h_kv, 2, d] dtype (in/out), 16-byte aligned.
+ */
+int swa_paged_bounds(const swa_paged_params *params, int32_t n_rows, const int32_t *slot, const void *k_pages, const float *k_scale,
+                     void *bounds, void *workspace, void *stream);
+
+/*
+ * score[s][h][j] = max over the query heads of key head h of scale * sum_c (max(q_c, 0) * hi_c + min(q_c, 0) * lo_c), for the pages j of sequence s that hold
+ * tokens: at least every logit of the page's keys (with SWA_KV_INT8: of keys rounded to dtype).  Accumulated in fp32.  What is no number (a key or query
+ * that is not finite) scores +inf, a page outside the pool -inf, and sets the SWA_ERR_BAD_REQUEST bit.  Other entries are left as they were.
+ * Sequences are left out as by the attention; one longer than its table or a stated len_bound sets the SWA_ERR_CAPACITY bit.
+ *   q [n_rows, h_q, d], bounds, block_table, cache_len (in); score [b, h_kv, max_pages] float32 (out).
+ */
+int swa_paged_score(const swa_paged_params *params, swa_rows q, int32_t n_rows, const int32_t *row_start, const int32_t *slot,
+                    const void *bounds, const int32_t *block_table, const int32_t *cache_len, float *score, void *workspace,
+                    void *stream);
+
+/*
+ * Of each sequence's pages that hold tokens: all where they are n_sel or fewer; else the `first` first ones, the `last` last ones, and of those between
+ * as many of highest score as make n_sel (ties: the lowest page; what is no number counts as +inf).  The scores may be any, swa_paged_score's or others.
+ * sel gets their numbers within the sequence in ascending order, and -1 behind them, sel_cnt how many there are.  A sequence with a negative
+ * cache_len has none, nor has one longer than its table or a stated len_bound, which sets the SWA_ERR_CAPACITY bit.
+ *   score [b, h_kv, max_pages] float32, cache_len [b] (in); sel [b, h_kv, n_sel], sel_cnt [b, h_kv] int32 (out);
+ *   1 <= n_sel <= max_pages, 0 <= first, 0 <= last, first + last <= n_sel.
+ */
+int swa_paged_select(const swa_paged_params *params, const float *score, const int32_t *cache_len, int32_t n_sel, int32_t first,
+                     int32_t last, int32_t *sel, int32_t *sel_cnt, void *workspace, void *stream);
+
+/*
+ * swa_paged_decode over the tokens of listed pages alone: those of pages sel[s][h][0 .. sel_cnt[s][h]) for the query heads of key head h.  lse is theirs, too.
+ * Entries below zero, and those of pages without tokens, count for nothing; entries of max_pages and more, pages outside the pool and a sel_cnt outside
+ * 0..n_sel (which counts as the nearer end) set the SWA_ERR_BAD_REQUEST bit.  A page listed twice counts twice.  Without tokens, out = 0 and lse = -inf.
+ * Everything else is as there, the roundings and skipped sequences too; the launch goes by n_sel * page_size tokens.
+ */
+int swa_paged_decode_selected(const swa_paged_params *params, swa_rows q, int32_t n_rows, const int32_t *row_start, const int32_t *slot,
+                              const void *k_pages, const void *v_pages, const float *k_scale, const float *v_scale,
+                              const int32_t *block_table, const int32_t *cache_len, const int32_t *sel, const int32_t *sel_cnt,
+                              int32_t n_sel, void *out, float *lse, void *workspace, void *stream);
+
+/*
+ * swa_paged_decode where sequences share prefixes: the tokens of sequence s are those of sequence prefix_of[s], then its own (prefix_of[s] = -1: its own
+ * alone).  A prefix is a sequence of the same cache, planned and appended like any other, of which further rows of the table need no copy; its keys and
+ * values are read once for all the sequences behind it, not once for each.  Positions that swa_paged_plan gives count a sequence's own tokens, so the caller adds
+ * the prefix's length to them before swa_paged_append.  A prefix that is kept and not decoded has no rows in row_start (new_cnt 0).
+ *   out[r] = softmax over the tokens of both, lse likewise; r, row_start, slot and skipped sequences as in swa_paged_decode_selected.
+ * One prefix counts: prefix_of[prefix_of[s]] is not looked at.  Sequences whose prefix is none (outside 0..b-1, s itself, or an unused row with a negative
+ * cache_len) are skipped and set the SWA_ERR_BAD_REQUEST bit; those of a prefix that is longer than its table or a stated len_bound are skipped and set the
+ * SWA_ERR_CAPACITY bit.  params->window is 0.  Roundings as in swa_paged_decode; a sequence's results may differ in their last bits with the call's others, whose
+ * lengths and prefixes say where tokens are cut into pieces.
+ * SWA_ERR_CAPACITY also for more than a launch holds: 2^24 of b * h_q, and about 2^31 of h_kv * (2 b + b * h_q / h_kv / 32) * len / 128 with len the
+ * longest sequence (of its table, len_bound).
+ *   prefix_of [b] int32 (in).
+ */
+int swa_paged_decode_shared(const swa_paged_params *params, swa_rows q, int32_t n_rows, const int32_t *row_start, const int32_t *slot,
+                            const void *k_pages, const void *v_pages, const float *k_scale, const float *v_scale,
+                            const int32_t *block_table, const int32_t *cache_len, const int32_t *prefix_of, void *out, float *lse,
+                            void *workspace, void *stream);
+
+/*
  * Measurement aid, not part of the method: reads `bytes` (rounded down to a multiple of 104 KiB)
  * from src with plain streaming 128-bit loads and discards them.  Timing it on a buffer much larger
  * than the caches gives the streaming-read ceiling of the machine, the practical denominator next

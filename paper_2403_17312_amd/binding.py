@@ -45,7 +45,7 @@ EXPORTS = ["swa_strerror", "swa_workspace_bytes", "swa_workspace_init", "swa_che
            "swa_decode_step_q8", "swa_prefill_rows", "swa_decode_step_window", "swa_prefill_attention", "swa_probe_stream_read",
            "swa_prepare", "swa_decode_step_static", "swa_decode_step_window_q8", "swa_offload_evicted", "swa_reload_tokens",
            "swa_paged_workspace_bytes", "swa_paged_workspace_init", "swa_paged_check_status", "swa_paged_plan", "swa_paged_append", "swa_paged_decode",
-           "swa_paged_decode_planned"]
+           "swa_paged_decode_planned", "swa_paged_bounds", "swa_paged_score", "swa_paged_select", "swa_paged_decode_selected", "swa_paged_decode_shared"]
 
 
 class SwaParams(ctypes.Structure):
@@ -85,7 +85,8 @@ _native = None      # the native half (csrc/swa_native.cpp), bound to the entry 
 # not a plain tensor, an integer or None; the call then takes the general path below, with its errors.
 NATIVE = ("swa_decode_step", "swa_decode_step_q8", "swa_decode_step_window", "swa_decode_step_window_q8", "swa_decode_step_static",
           "swa_compact_kv", "swa_prefill_scores", "swa_prefill_rows", "swa_prefill_attention", "swa_quantize_kv",
-          "swa_paged_plan", "swa_paged_append", "swa_paged_decode", "swa_paged_decode_planned")
+          "swa_paged_plan", "swa_paged_append", "swa_paged_decode", "swa_paged_decode_planned", "swa_paged_bounds", "swa_paged_score",
+          "swa_paged_select", "swa_paged_decode_selected", "swa_paged_decode_shared")
 
 
 class _General:
@@ -172,6 +173,16 @@ def lib():
         L.swa_paged_decode.argtypes = [gp, SwaRows, ctypes.c_int32] + [vp] * 11
         L.swa_paged_decode_planned.restype = ctypes.c_int
         L.swa_paged_decode_planned.argtypes = [gp, SwaRows, ctypes.c_int32] + [vp] * 12
+        L.swa_paged_bounds.restype = ctypes.c_int
+        L.swa_paged_bounds.argtypes = [gp, ctypes.c_int32] + [vp] * 6
+        L.swa_paged_score.restype = ctypes.c_int
+        L.swa_paged_score.argtypes = [gp, SwaRows, ctypes.c_int32] + [vp] * 8
+        L.swa_paged_select.restype = ctypes.c_int
+        L.swa_paged_select.argtypes = [gp] + [vp] * 2 + [ctypes.c_int32] * 3 + [vp] * 4
+        L.swa_paged_decode_selected.restype = ctypes.c_int
+        L.swa_paged_decode_selected.argtypes = [gp, SwaRows, ctypes.c_int32] + [vp] * 10 + [ctypes.c_int32] + [vp] * 4
+        L.swa_paged_decode_shared.restype = ctypes.c_int
+        L.swa_paged_decode_shared.argtypes = [gp, SwaRows, ctypes.c_int32] + [vp] * 13
         _lib, _native = L, _native_half(L)
     return _lib
 
@@ -483,6 +494,59 @@ def swa_paged_decode_planned(params: SwaPagedParams, q, n_rows: int, row_start, 
             _gpu_ptr(out), _gpu_ptr(lse), _gpu_ptr(workspace), _stream(stream))
     if rc != SWA_OK:
         raise SwaError(rc, "swa_paged_decode_planned")
+
+
+def swa_paged_bounds(params: SwaPagedParams, n_rows: int, slot, k_pages, k_scale, bounds, workspace, stream=None) -> None:
+    rc = _fast().swa_paged_bounds(params, n_rows, slot, k_pages, k_scale, bounds, workspace, stream)
+    if rc is None:
+        rc = lib().swa_paged_bounds(ctypes.byref(params), int(n_rows), _gpu_ptr(slot), _gpu_ptr(k_pages), _gpu_ptr(k_scale), _gpu_ptr(bounds),
+            _gpu_ptr(workspace), _stream(stream))
+    if rc != SWA_OK:
+        raise SwaError(rc, "swa_paged_bounds")
+
+
+def swa_paged_score(params: SwaPagedParams, q, n_rows: int, row_start, slot, bounds, block_table, cache_len, score, workspace,
+                    stream=None) -> None:
+    rc = _fast().swa_paged_score(params, q, n_rows, row_start, slot, bounds, block_table, cache_len, score, workspace, stream)
+    if rc is None:
+        rc = lib().swa_paged_score(ctypes.byref(params), _rows(q), int(n_rows), _gpu_ptr(row_start), _gpu_ptr(slot), _gpu_ptr(bounds),
+            _gpu_ptr(block_table), _gpu_ptr(cache_len), _gpu_ptr(score), _gpu_ptr(workspace), _stream(stream))
+    if rc != SWA_OK:
+        raise SwaError(rc, "swa_paged_score")
+
+
+def swa_paged_select(params: SwaPagedParams, score, cache_len, n_sel: int, first: int, last: int, sel, sel_cnt, workspace,
+                     stream=None) -> None:
+    rc = _fast().swa_paged_select(params, score, cache_len, n_sel, first, last, sel, sel_cnt, workspace, stream)
+    if rc is None:
+        rc = lib().swa_paged_select(ctypes.byref(params), _gpu_ptr(score), _gpu_ptr(cache_len), int(n_sel), int(first), int(last),
+            _gpu_ptr(sel), _gpu_ptr(sel_cnt), _gpu_ptr(workspace), _stream(stream))
+    if rc != SWA_OK:
+        raise SwaError(rc, "swa_paged_select")
+
+
+def swa_paged_decode_selected(params: SwaPagedParams, q, n_rows: int, row_start, slot, k_pages, v_pages, k_scale, v_scale, block_table,
+                              cache_len, sel, sel_cnt, n_sel: int, out, lse, workspace, stream=None) -> None:
+    rc = _fast().swa_paged_decode_selected(params, q, n_rows, row_start, slot, k_pages, v_pages, k_scale, v_scale, block_table, cache_len,
+        sel, sel_cnt, n_sel, out, lse, workspace, stream)
+    if rc is None:
+        rc = lib().swa_paged_decode_selected(ctypes.byref(params), _rows(q), int(n_rows), _gpu_ptr(row_start), _gpu_ptr(slot),
+            _gpu_ptr(k_pages), _gpu_ptr(v_pages), _gpu_ptr(k_scale), _gpu_ptr(v_scale), _gpu_ptr(block_table), _gpu_ptr(cache_len),
+            _gpu_ptr(sel), _gpu_ptr(sel_cnt), int(n_sel), _gpu_ptr(out), _gpu_ptr(lse), _gpu_ptr(workspace), _stream(stream))
+    if rc != SWA_OK:
+        raise SwaError(rc, "swa_paged_decode_selected")
+
+
+def swa_paged_decode_shared(params: SwaPagedParams, q, n_rows: int, row_start, slot, k_pages, v_pages, k_scale, v_scale, block_table,
+                            cache_len, prefix_of, out, lse, workspace, stream=None) -> None:
+    rc = _fast().swa_paged_decode_shared(params, q, n_rows, row_start, slot, k_pages, v_pages, k_scale, v_scale, block_table, cache_len,
+        prefix_of, out, lse, workspace, stream)
+    if rc is None:
+        rc = lib().swa_paged_decode_shared(ctypes.byref(params), _rows(q), int(n_rows), _gpu_ptr(row_start), _gpu_ptr(slot),
+            _gpu_ptr(k_pages), _gpu_ptr(v_pages), _gpu_ptr(k_scale), _gpu_ptr(v_scale), _gpu_ptr(block_table), _gpu_ptr(cache_len),
+            _gpu_ptr(prefix_of), _gpu_ptr(out), _gpu_ptr(lse), _gpu_ptr(workspace), _stream(stream))
+    if rc != SWA_OK:
+        raise SwaError(rc, "swa_paged_decode_shared")
 
 
 class PagedCache:

@@ -15,7 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB_PATH = os.path.join(HERE, "libswa_hip.so")
 NATIVE_PATH = os.path.join(HERE, "_swa_native.so")
 SOURCES = ["swa_api.hip", "swa_decode.hip", "swa_short.hip", "swa_short_shared.hip", "swa_compact.hip", "swa_prefill.hip", "swa_quant.hip", "swa_flash.hip", "swa_offload.hip", "swa_splitk.hip",
-           "swa_paged_api.hip", "swa_paged_plan.hip", "swa_paged_append.hip", "swa_paged_decode.hip"]
+           "swa_paged_api.hip", "swa_paged_plan.hip", "swa_paged_append.hip", "swa_paged_decode.hip",
+           "swa_paged_bounds.hip", "swa_paged_score.hip", "swa_paged_select.hip", "swa_paged_selected.hip", "swa_paged_shared.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -27,7 +28,8 @@ FLAGS = [
 
 # MFMA kernels: keep the accumulators in ordinary vector registers (no copies in and out of the
 # accumulation file around every softmax step).
-EXTRA = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for f in ("swa_flash.hip", "swa_prefill.hip", "swa_paged_decode.hip")}
+EXTRA = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for f in ("swa_flash.hip", "swa_prefill.hip", "swa_paged_decode.hip", "swa_paged_score.hip",
+                                                                         "swa_paged_selected.hip", "swa_paged_shared.hip")}
 
 
 def _compile(src: str) -> str:

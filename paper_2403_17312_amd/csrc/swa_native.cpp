@@ -158,7 +158,12 @@ struct Entry<int (*)(const P*, A...)> {
     X(swa_paged_plan) \
     X(swa_paged_append) \
     X(swa_paged_decode) \
-    X(swa_paged_decode_planned)
+    X(swa_paged_decode_planned) \
+    X(swa_paged_bounds) \
+    X(swa_paged_score) \
+    X(swa_paged_select) \
+    X(swa_paged_decode_selected) \
+    X(swa_paged_decode_shared)
 
 #define SWA_DEFINE(name) \
     void* addr_##name = nullptr; \

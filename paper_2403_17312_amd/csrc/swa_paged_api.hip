@@ -59,6 +59,15 @@ static int decode_call(const swa_paged_params* params, const swa_rows& q, int32_
                                workspace, static_cast<hipStream_t>(stream));
 }
 
+// What the calls with queries ask of them and of the lists that say whose they are.
+static int check_queries(const swa_paged_params& p, const swa_rows& q, int32_t n_rows, const int32_t* row_start, const int32_t* slot)
+{
+    if (slot && !row_start) return SWA_ERR_NULL;
+    const int rc = check_rows(p, q, p.h_q);
+    if (rc != SWA_OK) return rc;
+    return n_rows < 1 || n_rows > kMaxPlanRows || (!row_start && n_rows < p.b) ? SWA_ERR_BAD_SHAPE : SWA_OK;
+}
+
 __global__ void swa_paged_zero_kernel(int32_t* p)
 {
     if (threadIdx.x < 16) p[threadIdx.x] = 0;
@@ -71,7 +80,8 @@ extern "C" {
 size_t swa_paged_workspace_bytes(const swa_paged_params* params)
 {
     if (swa::validate_paged(params) != SWA_OK) return 0;
-    return (swa::kPagedPartialOffset + swa::paged_partial_bytes(*params) + 255) & ~(size_t)255;
+    const size_t decode = swa::paged_partial_bytes(*params), shared = swa::paged_shared_bytes(*params);
+    return (swa::kPagedPartialOffset + (decode > shared ? decode : shared) + 255) & ~(size_t)255;
 }
 
 int swa_paged_workspace_init(const swa_paged_params* params, void* workspace, void* stream)
@@ -150,6 +160,72 @@ int swa_paged_decode_planned(const swa_paged_params* params, swa_rows q, int32_t
     if (!row_start || !slot) return SWA_ERR_NULL;
     return swa::decode_call(params, q, n_rows, row_start, slot, k_pages, v_pages, k_scale, v_scale, block_table, cache_len, out, lse,
                             workspace, stream);
+}
+
+int swa_paged_bounds(const swa_paged_params* params, int32_t n_rows, const int32_t* slot, const void* k_pages, const float* k_scale, void* bounds,
+                     void* workspace, void* stream)
+{
+    const int rc = swa::validate_paged(params);
+    if (rc != SWA_OK) return rc;
+    if (!slot || !k_pages || (swa::paged_int8(*params) && !k_scale) || !bounds || !workspace) return SWA_ERR_NULL;
+    if (n_rows < 1 || n_rows > swa::kMaxPlanRows) return SWA_ERR_BAD_SHAPE;
+    if (!swa::on16(k_pages) || (swa::paged_int8(*params) && !swa::on16(k_scale)) || !swa::on16(bounds) || !swa::on16(workspace)) return SWA_ERR_ALIGNMENT;
+    return swa::launch_paged_bounds(*params, n_rows, slot, k_pages, k_scale, bounds, workspace, static_cast<hipStream_t>(stream));
+}
+
+int swa_paged_score(const swa_paged_params* params, swa_rows q, int32_t n_rows, const int32_t* row_start, const int32_t* slot, const void* bounds,
+                    const int32_t* block_table, const int32_t* cache_len, float* score, void* workspace, void* stream)
+{
+    int rc = swa::validate_paged(params);
+    if (rc != SWA_OK) return rc;
+    if (!bounds || !block_table || !cache_len || !score || !workspace) return SWA_ERR_NULL;
+    if ((rc = swa::check_queries(*params, q, n_rows, row_start, slot)) != SWA_OK) return rc;
+    if (params->window != 0) return SWA_ERR_BAD_SHAPE;
+    if (!swa::on16(bounds) || !swa::on16(workspace)) return SWA_ERR_ALIGNMENT;
+    return swa::launch_paged_score(*params, q, n_rows, row_start, slot, bounds, block_table, cache_len, score, workspace,
+                                   static_cast<hipStream_t>(stream));
+}
+
+int swa_paged_select(const swa_paged_params* params, const float* score, const int32_t* cache_len, int32_t n_sel, int32_t first, int32_t last,
+                     int32_t* sel, int32_t* sel_cnt, void* workspace, void* stream)
+{
+    const int rc = swa::validate_paged(params);
+    if (rc != SWA_OK) return rc;
+    if (!score || !cache_len || !sel || !sel_cnt || !workspace) return SWA_ERR_NULL;
+    if (n_sel < 1 || n_sel > params->max_pages || first < 0 || last < 0 || first > n_sel - last || params->window != 0) return SWA_ERR_BAD_SHAPE;
+    if (!swa::on16(workspace)) return SWA_ERR_ALIGNMENT;
+    return swa::launch_paged_select(*params, score, cache_len, n_sel, first, last, sel, sel_cnt, workspace, static_cast<hipStream_t>(stream));
+}
+
+int swa_paged_decode_selected(const swa_paged_params* params, swa_rows q, int32_t n_rows, const int32_t* row_start, const int32_t* slot,
+                              const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale, const int32_t* block_table,
+                              const int32_t* cache_len, const int32_t* sel, const int32_t* sel_cnt, int32_t n_sel, void* out, float* lse,
+                              void* workspace, void* stream)
+{
+    int rc = swa::validate_paged(params);
+    if (rc != SWA_OK) return rc;
+    if (!block_table || !cache_len || !sel || !sel_cnt || !out || !workspace) return SWA_ERR_NULL;
+    if ((rc = swa::check_pool(*params, k_pages, v_pages, k_scale, v_scale)) != SWA_OK) return rc;
+    if ((rc = swa::check_queries(*params, q, n_rows, row_start, slot)) != SWA_OK) return rc;
+    if (n_sel < 1 || n_sel > params->max_pages || params->window != 0) return SWA_ERR_BAD_SHAPE;
+    if (!swa::on16(out) || !swa::on16(workspace)) return SWA_ERR_ALIGNMENT;
+    return swa::launch_paged_selected(*params, q, n_rows, row_start, slot, k_pages, v_pages, k_scale, v_scale, block_table, cache_len, sel,
+                                      sel_cnt, n_sel, out, lse, workspace, static_cast<hipStream_t>(stream));
+}
+
+int swa_paged_decode_shared(const swa_paged_params* params, swa_rows q, int32_t n_rows, const int32_t* row_start, const int32_t* slot,
+                            const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale, const int32_t* block_table,
+                            const int32_t* cache_len, const int32_t* prefix_of, void* out, float* lse, void* workspace, void* stream)
+{
+    int rc = swa::validate_paged(params);
+    if (rc != SWA_OK) return rc;
+    if (!block_table || !cache_len || !prefix_of || !out || !workspace) return SWA_ERR_NULL;
+    if ((rc = swa::check_pool(*params, k_pages, v_pages, k_scale, v_scale)) != SWA_OK) return rc;
+    if ((rc = swa::check_queries(*params, q, n_rows, row_start, slot)) != SWA_OK) return rc;
+    if (params->window != 0) return SWA_ERR_BAD_SHAPE;
+    if (!swa::on16(out) || !swa::on16(workspace)) return SWA_ERR_ALIGNMENT;
+    return swa::launch_paged_shared(*params, q, n_rows, row_start, slot, k_pages, v_pages, k_scale, v_scale, block_table, cache_len, prefix_of,
+                                    out, lse, workspace, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

@@ -9,18 +9,9 @@
 //            holds whole sequences and at most two pieces.  128 sequences of 512 to 8192 tokens, 8 key heads of 128 bf16 channels: chunks
 //            425 us, shares 353 (6.5 TB/s).
 // Pieces leave partial results, which a second, small launch joins in their order.
-// All products go to the matrix cores, whose 16 columns are the query heads: also a single head's, since at their peak they are done in a fifteenth of the
-// time that HBM takes for 16 bits, a seventh for codes, and in fp32 something more than a third (with 32 columns: twice those parts).
-//   logits   S^T = K Q^T: a lane's operand is 16 bytes of one key, as it lies in memory; a 64-byte piece of 16 keys a load.
-//   values   O^T = V^T P^T: S^T leaves lane (j, c) with keys 4j..4j+3 of column c, which is what the product with V takes from that lane
-//            if its contraction runs over the keys in that order; nothing moves between lanes.  For V^T a lane loads the same D / 16
-//            channels of those keys (whole rows a load) and swaps halves of words, a byte permutation for two elements.
-// Tiles go from memory to registers and need no LDS.
-#include <math.h>
-
-#include <type_traits>
-
-#include "swa_paged.hpp"
+// All products go to the matrix cores, whose 16 columns are the query heads (swa_paged_tile.hpp): also a single head's, since at their peak they are done in a
+// fifteenth of the time that HBM takes for 16 bits, a seventh for codes, and in fp32 something more than a third (with 32 columns: twice those parts).
+#include "swa_paged_tile.hpp"
 
 namespace swa {
 
@@ -48,13 +39,7 @@ struct PagedArgs {
 };
 
 constexpr int kPagedWaves = 4;
-constexpr int kPagedStep = 128;                    // tokens
 constexpr int kPagedChunks = 256;                  // chunks of a sequence at most, which bounds what the join of one has to read
-
-// Query heads of a workgroup: the matrix cores' 16 columns, or twice as many, so that keys and values shared by more heads are read half as often.
-static int tile_heads_of(const swa_paged_params& p) { return p.h_q / p.h_kv > 16 ? 32 : 16; }
-
-static int row_tiles_of(const swa_paged_params& p) { return (p.h_q / p.h_kv + tile_heads_of(p) - 1) / tile_heads_of(p); }
 
 // Tokens of a sequence that a call may see, from a multiple of 32 on.
 static int64_t paged_span(const swa_paged_params& p)
@@ -112,66 +97,11 @@ size_t paged_partial_bytes(const swa_paged_params& p)
     return (size_t)paged_piece_rows(p) * (p.d + 2) * sizeof(float) + (size_t)paged_max_shares(p) * sizeof(int4);
 }
 
-typedef float f32x4_t __attribute__((ext_vector_type(4)));
-
-template <typename C>
-__device__ __forceinline__ f32x4_t mfma16(const Vec16& a, const Vec16& b, f32x4_t c)
+void paged_partials(const swa_paged_params& p, void* workspace, float*& out, float*& sum)
 {
-    if constexpr (std::is_same_v<C, F16>)
-        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
-    else if constexpr (std::is_same_v<C, BF16>)
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
-    else {
-        c = __builtin_amdgcn_mfma_f32_16x16x4f32(u2f(a.x), u2f(b.x), c, 0, 0, 0);
-        c = __builtin_amdgcn_mfma_f32_16x16x4f32(u2f(a.y), u2f(b.y), c, 0, 0, 0);
-        c = __builtin_amdgcn_mfma_f32_16x16x4f32(u2f(a.z), u2f(b.z), c, 0, 0, 0);
-        return __builtin_amdgcn_mfma_f32_16x16x4f32(u2f(a.w), u2f(b.w), c, 0, 0, 0);
-    }
+    out = reinterpret_cast<float*>(static_cast<char*>(workspace) + kPagedPartialOffset);
+    sum = out + paged_piece_rows(p) * p.d;
 }
-
-template <typename M>
-__device__ __forceinline__ uint32_t round2(float lo, float hi)
-{
-    if constexpr (std::is_same_v<M, F16>) return f32x2_to_f16x2_bits(lo, hi);
-    else return f32x2_to_bf16x2_bits(lo, hi);
-}
-
-// Eight weights (0 or more) as two numbers of the matrix cores' type each, big and rest.
-//   CODES: rounded to the nearest both times.
-//   else: the values may be infinite, and a weight's two numbers have to be 0 or of its sign for an infinity to stay one.  So big is cut off, from what lies just below the
-//   weight (bf16), or rest is raised to fp16's smallest number (2^-39 of the largest weight; not for a weight of 0).
-template <typename P, bool CODES>
-__device__ __forceinline__ void split8(const float* w, Vec16& big, Vec16& rest)
-{
-    float f[8], r[8];
-    if constexpr (CODES) {
-        big = Vec16{round2<P>(w[0], w[1]), round2<P>(w[2], w[3]), round2<P>(w[4], w[5]), round2<P>(w[6], w[7])};
-    } else if constexpr (std::is_same_v<P, F16>) {
-        auto cut = [&](int i) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(w[i], w[i + 1])); };
-        big = Vec16{cut(0), cut(2), cut(4), cut(6)};
-    } else {
-        auto below = [&](int i) { return __builtin_elementwise_sub_sat(f2u(w[i]), 1u); };
-        auto cut = [&](int i) { return __builtin_amdgcn_perm(below(i + 1), below(i), 0x07060302u); };
-        big = Vec16{cut(0), cut(2), cut(4), cut(6)};
-    }
-    unpack<P>(big, f);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        r[i] = w[i] - f[i];
-        if constexpr (!CODES && std::is_same_v<P, F16>) r[i] = fmaxf(r[i], fminf(w[i], 0x1p-24f));
-    }
-    rest = Vec16{round2<P>(r[0], r[1]), round2<P>(r[2], r[3]), round2<P>(r[4], r[5]), round2<P>(r[6], r[7])};
-}
-
-template <typename V>
-__device__ __forceinline__ V load_values(const char* p)
-{
-    typedef uint32_t words_t __attribute__((ext_vector_type(sizeof(V) / 4)));
-    if constexpr (sizeof(V) == 4) return V{{__builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(p))}};
-    else return __builtin_bit_cast(V, __builtin_nontemporal_load(reinterpret_cast<const words_t*>(p)));
-}
-
-__device__ __forceinline__ float code(uint32_t w, int i) { return (float)(int8_t)(w >> (8 * i)); }
 
 // What a sequence asks of this call: its row, its tokens lo .. n-1, and steps (0: nothing).
 __device__ __forceinline__ int paged_sequence(const PagedArgs& a, int s, int& row, int& lo, int& n, bool& too_long)
@@ -230,17 +160,8 @@ struct Shares {
 template <typename T, typename C, int D, bool SHARES, int ROWS, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, paged_two(Elem<C>::kBytes * D, ROWS, D) ? 2 : 3) swa_paged_decode_kernel(PagedArgs a)
 {
-    constexpr bool kCodes = std::is_same_v<C, Q8>, kWide = std::is_same_v<C, F32>;
-    // Codes are exact in either 16-bit type.  Keys get the queries' type; values get bf16, whose range the weights need, which are products with a
-    // scale there.  In 16 bits weights go as two numbers, which hold 15 or 16 bits in bf16 and 21 in fp16: one alone left the output a tenth to a quarter farther from
-    // the exact one than its own rounding does, and the second product is free (decode of 128 ragged sequences, bf16, 353.7 / 353.0 us, of one of 131071 tokens, fp16, 51.6 / 51.8).
-    constexpr int kTiles = kWide && (D == 128 || ROWS == 2) ? 1 : 2, kKeys = 16 * kTiles, kRow = D * Elem<C>::kBytes;
-    constexpr int kSteps = kWide ? D / 16 : D / 32;      // operands of a logit
-    constexpr int kChannels = D / 16;                    // of V in a lane
-    // A weight is exp2(x - top + kRaise).  fp16 has 2^-14 to 2^15 for normal numbers: raised so far the largest weight is 2^15 and half a step of
-    // the smallest numbers 2^-40 of it.  Without, a wave lost what lies 17.4 nats below its loudest token, which for 131072 such tokens beside one
-    // of small value was 6.7 % of the output.  The sum carries the same factor, so nothing takes it back but the maximum, as it is handed on.
-    constexpr float kRaise = std::is_same_v<C, F16> ? 15.f : 0.f;
+    typedef PagedTile<T, C, D, ROWS> S;
+    constexpr int kKeys = S::kKeys, kSteps = S::kSteps, kChannels = S::kChannels;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, j = lane >> 4;
 
     // Row tiles of one range read the same pages: eight ranges, then the same ones' next row tile, so that they meet in one XCD's L2.  Reads of HBM per
@@ -344,9 +265,7 @@ __global__ void __launch_bounds__(64 * WAVES, paged_two(Elem<C>::kBytes * D, ROW
             for (int g = 0; g < ROWS; ++g)
 #pragma unroll
                 for (int c = 0; c < kSteps; ++c) {
-                    // (16 bytes of codes are two operands' channels)
-                    const int at = kCodes ? (c / 2) * 64 + j * 16 + (c & 1) * 8 : kWide ? c * 16 + j * 4 : c * 32 + j * 8;
-                    q[g][c] = 16 * g + col < heads ? load16(from + (16 * g * D + at) * Elem<T>::kBytes) : Vec16{0u, 0u, 0u, 0u};
+                    q[g][c] = 16 * g + col < heads ? load16(from + 16 * g * D * Elem<T>::kBytes + S::query_at(c, j)) : Vec16{0u, 0u, 0u, 0u};
                 }
         }
 
@@ -382,167 +301,7 @@ __global__ void __launch_bounds__(64 * WAVES, paged_two(Elem<C>::kBytes * D, ROW
         };
         auto token_page = [&](int base) { return table[page_of(base)]; };
         auto token_off = [&](int base) { return base + (lane & (kKeys - 1)) - page_of(base) * a.page_size; };
-        constexpr int kLoads = kCodes ? D / 64 : kSteps, kVLoad = kWide ? D / 64 : 1, kVBytes = kWide ? 16 : kChannels * Elem<C>::kBytes;
-        struct alignas(kVBytes < 16 ? kVBytes : 16) Values { uint32_t w[kVBytes / 4]; };
-
-        // One tile, whose tokens lie in rows r (of lane t % kKeys) of the pool.  In `whole` tiles all of them do, and sixteen at a time behind each
-        // other, so that addresses are a scalar and a lane's constant; in others each lane fetches its rows' numbers, and rows of -1 are left out.
-        auto take = [&](auto whole, const int r) __attribute__((always_inline)) {
-            constexpr bool kWhole = decltype(whole)::value;
-            int rv[kTiles][4];
-            Vec16 k[kTiles][kLoads];
-            Values v[kTiles][4][kVLoad];
-            f32x4_t k_scale[kTiles], v_scale[kTiles];
-#pragma unroll
-            for (int u = 0; u < kTiles; ++u) {
-                const char* k_from;
-                if constexpr (kWhole) {
-                    const int64_t first = __builtin_amdgcn_readlane(r, u * 16);
-                    k_from = a.k_pages + first * kRow + (uint32_t)(col * kRow + j * 16);
-                } else {
-                    const int rk = __shfl(r, u * 16 + col, 64);
-                    k_from = a.k_pages + (int64_t)(rk < 0 ? 0 : rk) * kRow + j * 16;
-                }
-#pragma unroll
-                for (int c = 0; c < kLoads; ++c) k[u][c] = load16_stream(k_from + c * 64);
-            }
-#pragma unroll
-            for (int u = 0; u < kTiles; ++u) {
-                const int64_t first = kWhole ? __builtin_amdgcn_readlane(r, u * 16) : 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const char* v_from;
-                    if constexpr (kWhole) {
-                        v_from = a.v_pages + first * kRow + (uint32_t)(j * 4 * kRow + col * kVBytes) + i * kRow;
-                    } else {
-                        rv[u][i] = __shfl(r, u * 16 + j * 4 + i, 64);
-                        v_from = a.v_pages + (int64_t)(rv[u][i] < 0 ? 0 : rv[u][i]) * kRow + col * kVBytes;
-                    }
-#pragma unroll
-                    for (int x = 0; x < kVLoad; ++x) v[u][i][x] = load_values<Values>(v_from + x * 256);
-                }
-                if constexpr (kCodes) {
-                    if constexpr (kWhole) {
-                        k_scale[u] = *reinterpret_cast<const f32x4_t*>(a.k_scale + first + 4 * j);
-                        v_scale[u] = *reinterpret_cast<const f32x4_t*>(a.v_scale + first + 4 * j);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            k_scale[u][i] = rv[u][i] < 0 ? 0.f : a.k_scale[rv[u][i]];
-                            v_scale[u][i] = rv[u][i] < 0 ? 0.f : a.v_scale[rv[u][i]];
-                        }
-                    }
-                }
-            }
-
-            __builtin_amdgcn_sched_barrier(0);
-            float x[ROWS][kTiles][4];
-#pragma unroll
-            for (int u = 0; u < kTiles; ++u) {
-                f32x4_t logit[ROWS];
-#pragma unroll
-                for (int g = 0; g < ROWS; ++g) logit[g] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int c = 0; c < kSteps; ++c) {
-                    Vec16 op;
-                    if constexpr (kCodes) {
-                        const Vec16& b = k[u][c / 2];
-                        const uint32_t w[2] = {c & 1 ? b.z : b.x, c & 1 ? b.w : b.y};
-                        op = Vec16{round2<T>(code(w[0], 0), code(w[0], 1)), round2<T>(code(w[0], 2), code(w[0], 3)),
-                                   round2<T>(code(w[1], 0), code(w[1], 1)), round2<T>(code(w[1], 2), code(w[1], 3))};
-                    } else {
-                        op = k[u][c];
-                    }
-#pragma unroll
-                    for (int g = 0; g < ROWS; ++g) logit[g] = mfma16<T>(op, q[g][c], logit[g]);
-                }
-#pragma unroll
-                for (int g = 0; g < ROWS; ++g)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        x[g][u][i] = logit[g][i] * a.scale;
-                        if constexpr (kCodes) x[g][u][i] *= k_scale[u][i];
-                        if constexpr (!kWhole) x[g][u][i] = rv[u][i] < 0 ? -INFINITY : x[g][u][i];
-                    }
-            }
-            if constexpr (!kWhole) {                         // (a weight of 0 times what is no number is none either)
-#pragma unroll
-                for (int u = 0; u < kTiles; ++u)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t keep = rv[u][i] < 0 ? 0u : ~0u;
-#pragma unroll
-                        for (int y = 0; y < kVLoad; ++y)
-#pragma unroll
-                            for (int z = 0; z < kVBytes / 4; ++z) v[u][i][y].w[z] &= keep;
-                    }
-            }
-#pragma unroll
-            for (int g = 0; g < ROWS; ++g) {
-                float most = x[g][0][0];
-#pragma unroll
-                for (int i = 1; i < 4 * kTiles; ++i) most = fmaxf(most, x[g][i / 4][i % 4]);
-                most = fmaxf(most, __shfl_xor(most, 16, 64));
-                most = fmaxf(most, __shfl_xor(most, 32, 64));
-                if (__any(most > top[g])) {
-                    const float to = fmaxf(top[g], most), down = __builtin_amdgcn_exp2f(top[g] - (to == -INFINITY ? 0.f : to));
-                    top[g] = to;
-                    sum[g] *= down;
-#pragma unroll
-                    for (int e = 0; e < kChannels; ++e) acc[g][e] *= down;
-                }
-                const float from = (top[g] == -INFINITY ? 0.f : top[g]) - kRaise;
-#pragma unroll
-                for (int u = 0; u < kTiles; ++u)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        x[g][u][i] = __builtin_amdgcn_exp2f(x[g][u][i] - from);
-                        sum[g] += x[g][u][i];
-                        if constexpr (kCodes) x[g][u][i] *= v_scale[u][i];
-                    }
-            }
-
-            if constexpr (kWide) {
-#pragma unroll
-                for (int u = 0; u < kTiles; ++u)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int e = 0; e < kChannels; ++e)
-#pragma unroll
-                            for (int g = 0; g < ROWS; ++g)
-                                acc[g][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(u2f(v[u][i][e / 4].w[e % 4]), x[g][u][i], acc[g][e], 0, 0, 0);
-            } else {
-#pragma unroll
-                for (int u = 0; u < kTiles; u += 2) {        // 32 keys a product
-                    typedef std::conditional_t<kCodes, BF16, T> P;
-                    Vec16 p[ROWS], p_rest[ROWS];
-#pragma unroll
-                    for (int g = 0; g < ROWS; ++g) split8<P, kCodes>(x[g][u], p[g], p_rest[g]);
-#pragma unroll
-                    for (int e = 0; e < kChannels; ++e) {
-                        Vec16 op;
-                        if constexpr (kCodes) {
-                            auto c = [&](int w, int i) { return code(v[u + w][i][0].w[e / 4], e % 4); };
-                            op = Vec16{round2<BF16>(c(0, 0), c(0, 1)), round2<BF16>(c(0, 2), c(0, 3)), round2<BF16>(c(1, 0), c(1, 1)),
-                                       round2<BF16>(c(1, 2), c(1, 3))};
-                        } else {
-                            constexpr uint32_t kLow = 0x05040100u, kHigh = 0x07060302u;
-                            auto two = [&](int w, int i) {
-                                return __builtin_amdgcn_perm(v[u + w][i + 1][0].w[e / 2], v[u + w][i][0].w[e / 2], e & 1 ? kHigh : kLow);
-                            };
-                            op = Vec16{two(0, 0), two(0, 2), two(1, 0), two(1, 2)};
-                        }
-#pragma unroll
-                        for (int g = 0; g < ROWS; ++g) {
-                            acc[g][e] = mfma16<P>(op, p[g], acc[g][e]);
-                            acc[g][e] = mfma16<P>(op, p_rest[g], acc[g][e]);
-                        }
-                    }
-                }
-            }
-        };
-
+        const PagedPool pool{a.k_pages, a.v_pages, a.k_scale, a.v_scale, a.scale};
         // Whole tiles first; the others, at the ends of the window and where a page is not in the pool, in a loop of their own, whose addresses then
         // take no registers from this one.
         constexpr int kStride = WAVES * kKeys;
@@ -565,7 +324,7 @@ __global__ void __launch_bounds__(64 * WAVES, paged_two(Elem<C>::kBytes * D, ROW
                 if (next < end) page = token_page(next);
                 const int rows = row_of(base, this_page);
                 if (!__any(rows < 0)) {
-                    take(std::true_type{}, rows);
+                    paged_take<T, C, D, ROWS, true>(pool, rows, q, top, sum, acc);
                 } else {
                     if (left == end) {
                         left = base;
@@ -578,7 +337,7 @@ __global__ void __launch_bounds__(64 * WAVES, paged_two(Elem<C>::kBytes * D, ROW
             r = row_of(next, page);
         }
         while (left < left_end) {
-            take(std::false_type{}, r);
+            paged_take<T, C, D, ROWS, false>(pool, r, q, top, sum, acc);
             do {
                 left += kStride;
                 if (left >= left_end) break;
@@ -590,49 +349,18 @@ __global__ void __launch_bounds__(64 * WAVES, paged_two(Elem<C>::kBytes * D, ROW
         // The waves' results to one, in LDS: rows are query heads.
         int who = tid;
         if (SHARES) asm volatile("" : "+v"(who));            // (addresses made from it are not kept in registers around the loop)
-        const int to_col = who & 15, to_j = (who >> 4) & 3;
+        paged_join_waves<T, C, D, ROWS, WAVES>(part, tops, sums, top, sum, acc, heads, who, [&](int head, float all, float total, const float (&y)[kChannels]) __attribute__((always_inline)) {
+            if (whole) {
+                const int64_t at = (int64_t)row * a.h_q + head0 + head;
+                paged_store<T, D>(a.out, a.lse, at, (who & 15) * kChannels, (who & 15) == 0, all, total, y);
+            } else {
+                const int64_t at = (piece * a.row_tiles + tile) * a.heads + head;
 #pragma unroll
-        for (int g = 0; g < ROWS; ++g) {
-            sum[g] += __shfl_xor(sum[g], 16, 64);
-            sum[g] += __shfl_xor(sum[g], 32, 64);
-            __syncthreads();                                     // (what was there before has been read)
-            if (to_j == 0) {
-                tops[wave][to_col] = top[g] - kRaise;
-                sums[wave][to_col] = sum[g];
+                for (int e = 0; e < kChannels; e += 4)
+                    *reinterpret_cast<f32x4_t*>(a.part_out + at * D + (who & 15) * kChannels + e) = f32x4_t{y[e], y[e + 1], y[e + 2], y[e + 3]};
+                if ((who & 15) == 0) *reinterpret_cast<float2*>(a.part_sum + at * 2) = float2{all, total};
             }
-#pragma unroll
-            for (int e = 0; e < kChannels; ++e)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) part[wave][to_col][kWide ? (e / 4) * 64 + (4 * to_j + i) * 4 + e % 4 : (4 * to_j + i) * kChannels + e] = acc[g][e][i];
-            __syncthreads();
-            for (int head = who >> 4; head < 16 && 16 * g + head < heads; head += 4 * WAVES) {
-                float all = tops[0][head];
-#pragma unroll
-                for (int w = 1; w < WAVES; ++w) all = fmaxf(all, tops[w][head]);
-                float total = 0.f, y[kChannels] = {};
-#pragma unroll
-                for (int w = 0; w < WAVES; ++w) {
-                    const float f = __builtin_amdgcn_exp2f(tops[w][head] - (all == -INFINITY ? 0.f : all));
-                    total = __builtin_fmaf(sums[w][head], f, total);
-#pragma unroll
-                    for (int e = 0; e < kChannels; ++e) y[e] = __builtin_fmaf(part[w][head][(who & 15) * kChannels + e], f, y[e]);
-                }
-                if (whole) {
-                    const int64_t at = (int64_t)row * a.h_q + head0 + 16 * g + head;
-                    const float inverse = 1.f / total;
-                    char* const to = a.out + at * (D * Elem<T>::kBytes);
-#pragma unroll
-                    for (int e = 0; e < kChannels; ++e) store_elem<T>(to, (who & 15) * kChannels + e, total == 0.f ? 0.f : y[e] * inverse);
-                    if (a.lse && (who & 15) == 0) a.lse[at] = (all + __builtin_log2f(total)) * 0.69314718055994530942f;
-                } else {
-                    const int64_t at = (piece * a.row_tiles + tile) * a.heads + 16 * g + head;
-#pragma unroll
-                    for (int e = 0; e < kChannels; e += 4)
-                        *reinterpret_cast<f32x4_t*>(a.part_out + at * D + (who & 15) * kChannels + e) = f32x4_t{y[e], y[e + 1], y[e + 2], y[e + 3]};
-                    if ((who & 15) == 0) *reinterpret_cast<float2*>(a.part_sum + at * 2) = float2{all, total};
-                }
-            }
-        }
+        });
         if (SHARES && kv == a.h_kv - 1 && x == before[s + 1] * a.h_kv) ++s;
     } while (SHARES);
     if (SHARES && tile == 0 && tid == 0) a.begun[work] = begun;
@@ -760,6 +488,27 @@ static int launch_paged_form(const PagedArgs& a, bool in_shares, hipStream_t str
     return SWA_OK;
 }
 
+// Steps of a chunk, where a sequence has so many.
+// Work is even, so a call takes as long as the CU that has most of it.  us, as many chunks as make 1024 workgroups, 512, and by this rule (two
+// on a CU before three before one): 131071 tokens, 4 key heads, 16 query heads each 54.5 / 50.4 / 50.4; 6 sequences of 32000, 8 key heads 126.8 /
+// 155 (some CUs three) / 126.4; 2 of 10000, fp32 37.9 / 36.3 / 32.3.
+// And the join, whose launch is worth about a step (2 us), and another one with a thousand query heads to join: us, by these chunks without that / one
+// chunk, fp16, d = 128: 1 sequence, 8 key heads, 256 tokens 7.4 / 6.2, 384 7.5 / 7.8, 1000 8.3 / 20.2; 183 sequences of 16 query heads on one, 256 13.7 /
+// 8.2, 1000 23.1 / 20.1; 48 of 64 on 8, 512 21.8 / 17.9, 1000 32.5 / 30.9.
+int64_t paged_chunk_steps(const swa_paged_params& p, int64_t of_one)
+{
+    int64_t each = of_one, least = (paged_units(p) + 255) / 256 * of_one * 1024;     // steps of a chunk; of the CU that has most, in 1024ths
+    for (int k : {2, 3, 1}) {
+        const int64_t e = (of_one + paged_chunks(p, k) - 1) / paged_chunks(p, k), groups = paged_units(p) * ((of_one + e - 1) / e);
+        const int64_t most = (groups + 255) / 256 * e * 1024 + 1024 + (int64_t)p.b * p.h_q;
+        if (e < of_one && most < least) {
+            least = most;
+            each = e;
+        }
+    }
+    return each;
+}
+
 int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_rows, const int32_t* row_start, const int32_t* slot,
                         const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale, const int32_t* block_table,
                         const int32_t* cache_len, void* out, float* lse, void* workspace, hipStream_t stream)
@@ -786,8 +535,7 @@ int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_
     a.n_pages = p.n_pages;
     a.max_pages = p.max_pages;
     a.window = p.window;
-    a.len_max = p.max_pages * p.page_size;
-    if (p.len_bound > 0 && p.len_bound < a.len_max) a.len_max = p.len_bound;
+    a.len_max = paged_len_max(p);
     a.group = p.h_q / p.h_kv;
     a.tile_heads = tile_heads_of(p);
     a.row_tiles = row_tiles_of(p);
@@ -805,27 +553,11 @@ int launch_paged_decode(const swa_paged_params& p, const swa_rows& q, int32_t n_
     if (in_shares) {
         a.ranges = paged_max_shares(p);
     } else {
-        const int64_t of_one = steps / units;
-        // Work is even, so a call takes as long as the CU that has most of it.  us, as many chunks as make 1024 workgroups, 512, and by this rule (two
-        // on a CU before three before one): 131071 tokens, 4 key heads, 16 query heads each 54.5 / 50.4 / 50.4; 6 sequences of 32000, 8 key heads 126.8 /
-        // 155 (some CUs three) / 126.4; 2 of 10000, fp32 37.9 / 36.3 / 32.3.
-        // And the join, whose launch is worth about a step (2 us), and another one with a thousand query heads to join: us, by these chunks without that / one
-        // chunk, fp16, d = 128: 1 sequence, 8 key heads, 256 tokens 7.4 / 6.2, 384 7.5 / 7.8, 1000 8.3 / 20.2; 183 sequences of 16 query heads on one, 256 13.7 /
-        // 8.2, 1000 23.1 / 20.1; 48 of 64 on 8, 512 21.8 / 17.9, 1000 32.5 / 30.9.
-        int64_t each = of_one, least = (paged_units(p) + 255) / 256 * of_one * 1024;     // steps of a workgroup; of that CU, in 1024ths
-        for (int k : {2, 3, 1}) {
-            const int64_t e = (of_one + paged_chunks(p, k) - 1) / paged_chunks(p, k), groups = paged_units(p) * ((of_one + e - 1) / e);
-            const int64_t most = (groups + 255) / 256 * e * 1024 + 1024 + (int64_t)p.b * p.h_q;
-            if (e < of_one && most < least) {
-                least = most;
-                each = e;
-            }
-        }
+        const int64_t of_one = steps / units, each = paged_chunk_steps(p, of_one);
         a.chunk = (p.len_bound > 0 && each <= 8) || p.b > 64 ? (int32_t)(each * kPagedStep) : 0;
         a.ranges = (int32_t)((of_one + each - 1) / each);
     }
-    a.part_out = reinterpret_cast<float*>(static_cast<char*>(workspace) + kPagedPartialOffset);
-    a.part_sum = a.part_out + paged_piece_rows(p) * p.d;
+    paged_partials(p, workspace, a.part_out, a.part_sum);
     a.begun = reinterpret_cast<int4*>(a.part_sum + paged_piece_rows(p) * 2);
 
 #define SWA_PAGED(T, C) (p.d == 64 ? launch_paged_form<T, C, 64>(a, in_shares, stream) : launch_paged_form<T, C, 128>(a, in_shares, stream))
