@@ -597,6 +597,7 @@ int swa_paged_bounds(const swa_paged_params *params, int32_t n_rows, const int32
  * tokens: at least every logit of the page's keys (with SWA_KV_INT8: of keys rounded to dtype).  Accumulated in fp32.  What is no number (a key or query
  * that is not finite) scores +inf, a page outside the pool -inf, and sets the SWA_ERR_BAD_REQUEST bit.  Other entries are left as they were.
  * Sequences are left out as by the attention; one longer than its table or a stated len_bound sets the SWA_ERR_CAPACITY bit.
+ * SWA_ERR_CAPACITY also where b * h_kv times the pages that a sequence may have reaches 2^31.
  *   q [n_rows, h_q, d], bounds, block_table, cache_len (in); score [b, h_kv, max_pages] float32 (out).
  */
 int swa_paged_score(const swa_paged_params *params, swa_rows q, int32_t n_rows, const int32_t *row_start, const int32_t *slot,
@@ -609,7 +610,7 @@ int swa_paged_score(const swa_paged_params *params, swa_rows q, int32_t n_rows, 
  * sel gets their numbers within the sequence in ascending order, and -1 behind them, sel_cnt how many there are.  A sequence with a negative
  * cache_len has none, nor has one longer than its table or a stated len_bound, which sets the SWA_ERR_CAPACITY bit.
  *   score [b, h_kv, max_pages] float32, cache_len [b] (in); sel [b, h_kv, n_sel], sel_cnt [b, h_kv] int32 (out);
- *   1 <= n_sel <= max_pages, 0 <= first, 0 <= last, first + last <= n_sel.
+ *   1 <= n_sel <= max_pages, 0 <= first, 0 <= last, first + last <= n_sel; b * h_kv below 2^22 (SWA_ERR_CAPACITY).
  */
 int swa_paged_select(const swa_paged_params *params, const float *score, const int32_t *cache_len, int32_t n_sel, int32_t first,
                      int32_t last, int32_t *sel, int32_t *sel_cnt, void *workspace, void *stream);

@@ -104,7 +104,7 @@ int launch_paged_select(const swa_paged_params& p, const float* score, const int
                      n_sel, first, last};
     const int64_t pages = paged_pages_max(p);
     const dim3 grid((unsigned)((int64_t)p.b * p.h_kv));
-    if ((uint64_t)p.b * p.h_kv * (pages <= 2048 ? 256 : 1024) > 0xffffffffULL) return SWA_ERR_CAPACITY;
+    if ((int64_t)p.b * p.h_kv >= 1 << 22) return SWA_ERR_CAPACITY;                     // (threads of a launch)
     if (pages <= 2048) launch_kernel(swa_paged_select_kernel<256, 8>, grid, dim3(256), 0, stream, a);
     else if (pages <= 8192) launch_kernel(swa_paged_select_kernel<1024, 8>, grid, dim3(1024), 0, stream, a);
     else launch_kernel(swa_paged_select_kernel<1024, 0>, grid, dim3(1024), 0, stream, a);

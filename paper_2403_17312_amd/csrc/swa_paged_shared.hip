@@ -38,35 +38,7 @@ struct SharedArgs {
 
 constexpr int kNoPrefix = 0, kLeftOut = 0xffff;    // of a sequence, where it has no prefix or the call leaves it out; else the prefix's number and 1
 
-// The shares: the first `more` of them have one step more than the others.
-struct EvenShares {
-    int steps, more;
-    __device__ __forceinline__ EvenShares(int total, int shares) : steps(total / shares), more(total % shares) {}
-    __device__ __forceinline__ int begin(int g) const { return g * steps + (g < more ? g : more); }
-    __device__ __forceinline__ int of(int x) const
-    {
-        const int longer = more * (steps + 1);
-        return x < longer ? x / (steps + 1) : more + (x - longer) / steps;
-    }
-};
-
 __device__ __forceinline__ int steps_of(int tokens) { return (tokens + kPagedStep - 1) / kPagedStep; }
-
-// Sums of v up to and including every thread of a workgroup of 256 (scratch: 4 of LDS; all of them arrive).
-__device__ __forceinline__ int sum_to(int v, int* scratch)
-{
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int up = __shfl_up(v, o, 64);
-        if (lane >= o) v += up;
-    }
-    __syncthreads();
-    if (lane == 63) scratch[wave] = v;
-    __syncthreads();
-    for (int w = 0; w < wave; ++w) v += scratch[w];
-    return v;
-}
 
 // Tokens begin .. end - 1 of the pages in `table`, for query columns whose rows begin at from(g).
 template <typename T, typename C, int D, int ROWS, typename Q, typename F>
@@ -207,7 +179,7 @@ __global__ void __launch_bounds__(256, Elem<C>::kBytes * D == 512 && ROWS == 2 ?
     }
     __syncthreads();
     const int total = __builtin_amdgcn_readfirstlane(before[2 * b]) * a.h_kv;
-    const EvenShares shares(total, a.shares);
+    const PagedShares shares(total, a.shares);
     // what the join asks of this call: a wave has a sequence
     for (int s = blockIdx.x * 4 + (tid >> 6); s < b; s += gridDim.x * 4) {
         const int is = prefix[s];
@@ -295,7 +267,7 @@ __global__ void __launch_bounds__(256) swa_paged_join_shared_kernel(SharedArgs a
     const int s = blockIdx.x / a.h_q, hq = blockIdx.x - s * a.h_q, kv = hq / a.group, head = hq - kv * a.group;
     const SharedPlace at = a.place[s];
     if (at.row < 0) return;
-    const EvenShares shares(*reinterpret_cast<const int32_t*>(a.place + a.b), a.shares);
+    const PagedShares shares(*reinterpret_cast<const int32_t*>(a.place + a.b), a.shares);
     const int width = tile > own_tile ? tile : own_tile;
     int64_t first[2];
     int count[2] = {0, 0};

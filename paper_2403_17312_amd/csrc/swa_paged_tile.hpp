@@ -116,8 +116,39 @@ __device__ __forceinline__ bool paged_row(const PagedRows& a, int s, int& row, i
     }
     if (n < 0 || row < 0 || row >= a.n_rows) return false;
     if (a.slot && a.slot[row] < 0) return false;
-    too_long = n > a.len_max;
-    return !too_long;
+    if (n > a.len_max) {
+        too_long = true;
+        return false;
+    }
+    return true;
+}
+
+// The shares: the first `more` of them have one step more than the others.
+struct PagedShares {
+    int steps, more;
+    __device__ __forceinline__ PagedShares(int total, int shares) : steps(total / shares), more(total % shares) {}
+    __device__ __forceinline__ int begin(int g) const { return g * steps + (g < more ? g : more); }
+    __device__ __forceinline__ int of(int x) const
+    {
+        const int longer = more * (steps + 1);
+        return x < longer ? x / (steps + 1) : more + (x - longer) / steps;
+    }
+};
+
+// Sum of v up to and including this thread of a workgroup (scratch: one of LDS for each wave; all of them arrive).
+__device__ __forceinline__ int sum_to(int v, int* scratch)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int up = __shfl_up(v, o, 64);
+        if (lane >= o) v += up;
+    }
+    __syncthreads();
+    if (lane == 63) scratch[wave] = v;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) v += scratch[w];
+    return v;
 }
 
 // The pool, and the scale of logits to the base 2.

@@ -100,10 +100,10 @@ def test_more_than_a_launch_holds(B):  # noqa: F811
     q = B.SwaRows(ok, 16384 * p.d)
     assert selected(B, p, n=4096, q=q, n_sel=1) == B.SWA_ERR_CAPACITY
     assert shared(B, p, n=4096, q=q) == B.SWA_ERR_CAPACITY
-    assert score(B, p, n=4096, q=q) == B.SWA_ERR_CAPACITY
     assert select(B, p, 1, 0, 0) == B.SWA_ERR_CAPACITY
     p = params(B, b=64, h_q=8, h_kv=8, n_pages=1, max_pages=1 << 26)         # 2^30 tokens a sequence
     assert shared(B, p, n=64, q=B.SwaRows(ok, 512)) == B.SWA_ERR_CAPACITY
+    assert score(B, p, n=64, q=B.SwaRows(ok, 512)) == B.SWA_ERR_CAPACITY
 
 
 @pytest.mark.parametrize("general", [False, True])
