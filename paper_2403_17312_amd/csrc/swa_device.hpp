@@ -348,6 +348,17 @@ __device__ __forceinline__ uint32_t lds_address(const char* p)
     return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char*)p;
 }
 
+// Two transposing LDS reads as one 16-byte fragment.  ds_read_b64_tr_b16, within 16 lanes: lane j supplies the
+// address of row j/4, columns 4 (j%4) .. +3 of a 4x16 block and receives column j of its four rows.
+typedef short short4_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ Vec16 lds_read_tr(const char* lo, const char* hi)
+{
+    typedef __attribute__((address_space(3))) short4_t* ptr_t;
+    const uint2 x = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr_t)lo));
+    const uint2 y = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ptr_t)hi));
+    return Vec16{x.x, x.y, y.x, y.y};
+}
+
 // ---- wave / block reductions -------------------------------------------------
 
 // Cross-lane move on the VALU data-parallel-primitive path (no LDS traffic).
@@ -369,6 +380,17 @@ __device__ __forceinline__ float group_sum(float v)
     if (LANES >= 16) v += dpp_move<0x140>(v);   // row_mirror
     if (LANES >= 32) v += __shfl_xor(v, 16, 64);
     return v;
+}
+
+// x of lane (l % 32) and x of lane (l % 32) + 32, in every lane: v_permlane32_swap exchanges the
+// upper half of one register with the lower half of another, so two copies of x come back as
+// (the lower half's x, the upper half's x) - no trip through LDS.
+__device__ __forceinline__ void both_halves(float x, float& lo, float& hi)
+{
+    const uint32_t u = __float_as_uint(x);
+    const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    lo = __uint_as_float(r[0]);
+    hi = __uint_as_float(r[1]);
 }
 
 // Whole-wave reductions: four DPP steps inside each row of 16 lanes, then two LDS-routed

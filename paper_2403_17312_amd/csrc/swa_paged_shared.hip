@@ -40,13 +40,34 @@ constexpr int kNoPrefix = 0, kLeftOut = 0xffff;    // of a sequence, where it ha
 
 __device__ __forceinline__ int steps_of(int tokens) { return (tokens + kPagedStep - 1) / kPagedStep; }
 
-// Tokens begin .. end - 1 of the pages in `table`, for query columns whose rows begin at from(g).
-template <typename T, typename C, int D, int ROWS, typename Q, typename F>
-__device__ __forceinline__ void shared_part(const SharedArgs& a, const int32_t* table, int kv, int begin, int end, int columns, float (&part)[4][16][D + 4],
-                                            float (&tops)[4][16], float (&sums)[4][16], Q from, F emit)
+// A partial result, by sixteen threads.
+template <int D>
+struct SharedEmit {
+    float *part_out, *part_sum;
+    int64_t to;                                          // of column 0
+    __device__ __forceinline__ void operator()(int i, float all, float sum, const float (&y)[D / 16]) const
+    {
+        const int64_t at = to + i;
+        const int c = (threadIdx.x & 15) * (D / 16);
+#pragma unroll
+        for (int z = 0; z < D / 16; z += 4) *reinterpret_cast<f32x4_t*>(part_out + at * D + c + z) = f32x4_t{y[z], y[z + 1], y[z + 2], y[z + 3]};
+        if (c == 0) *reinterpret_cast<float2*>(part_sum + at * 2) = float2{all, sum};
+    }
+};
+
+// Results of waves on their way to one.
+template <int D, int WAVES>
+struct SharedLds {
+    float part[WAVES][16][D + 4];
+    float tops[WAVES][16], sums[WAVES][16];
+};
+
+// Tokens begin .. end - 1 of the pages in `table`, for query columns whose rows begin at from(column).
+template <typename T, typename C, int D, int ROWS, int WAVES, typename Q, typename F>
+__device__ __forceinline__ void shared_part(const SharedArgs& a, const int32_t* table, int kv, int begin, int end, int columns, SharedLds<D, WAVES>& lds, Q from, F emit)
 {
     typedef PagedTile<T, C, D, ROWS> S;
-    constexpr int kKeys = S::kKeys, kSteps = S::kSteps, kChannels = S::kChannels, kStride = 4 * kKeys;
+    constexpr int kKeys = S::kKeys, kSteps = S::kSteps, kChannels = S::kChannels, kStride = WAVES * kKeys;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, j = lane >> 4;
     Vec16 q[ROWS][kSteps];
 #pragma unroll
@@ -111,28 +132,34 @@ __device__ __forceinline__ void shared_part(const SharedArgs& a, const int32_t* 
     if (bad) atomicOr(a.status, kStatusBadRequestBit);
     int who = threadIdx.x;
     asm volatile("" : "+v"(who));                        // (addresses made from it are not kept in registers around the loop)
-    paged_join_waves<T, C, D, ROWS, 4>(part, tops, sums, top, sum, acc, columns, who, emit);
+    paged_join_waves<T, C, D, ROWS, WAVES>(lds.part, lds.tops, lds.sums, top, sum, acc, columns, who, emit);
 }
 
-// OWN: sixteens of columns in a unit of a sequence's own tokens, ROWS: of a prefix's.
-template <typename T, typename C, int D, int ROWS, int OWN>
-__global__ void __launch_bounds__(256, Elem<C>::kBytes * D == 512 && ROWS == 2 ? 1 : 2) swa_paged_shared_kernel(SharedArgs a)
+// What every workgroup sums up by itself, in LDS.
+struct SharedLists {
+    int* before;                                         // [2 b + 1]: steps of a key head before prefix e, and before sequence e - b
+    uint16_t *members, *prefix;                          // [b + 1]: sequences of the prefixes before; [b]: a sequence's own prefix
+    int* scratch;                                        // one for each wave
+    __device__ __forceinline__ SharedLists(int* lds, int b, int* scratch_) : before(lds), members(reinterpret_cast<uint16_t*>(lds + 2 * b + 1)), prefix(members + b + 1), scratch(scratch_) {}
+};
+constexpr size_t shared_lists_bytes(int64_t b) { return (sizeof(int) * (2 * b + 1) + sizeof(uint16_t) * (2 * b + 1) + 15) / 16 * 16; }
+
+// The lists, what the join asks of this call, and then this workgroup's share, prefixes by prefix_part and sequences by shared_part.
+//   TILE, OWN: columns of a unit of a prefix's tokens, sixteens of them in one of a sequence's own.
+template <typename T, typename C, int D, int TILE, int OWN, int WAVES, typename P>
+__device__ __forceinline__ void shared_share(const SharedArgs& a, const SharedLists& lists, int (&member_row)[TILE + 1], SharedLds<D, WAVES>& lds, P prefix_part)
 {
-    constexpr int kColumns = 16 * (ROWS > OWN ? ROWS : OWN), kOwn = 16 * OWN, kTile = 16 * ROWS;
-    __shared__ float part[4][16][D + 4];
-    __shared__ float tops[4][16], sums[4][16];
-    __shared__ int scratch[4], member_row[kTile + 1];
-    extern __shared__ int before[];                      // steps of a key head before prefix e, and before sequence e - b, for e <= 2 b
-    uint16_t* const members = reinterpret_cast<uint16_t*>(before + 2 * a.b + 1);     // sequences of the prefixes before, b + 1 of them
-    uint16_t* const prefix = members + a.b + 1;          // of a sequence
+    constexpr int kOwn = 16 * OWN, kColumns = TILE > kOwn ? TILE : kOwn, NT = 64 * WAVES;
+    int* const before = lists.before;
+    uint16_t *const members = lists.members, *const prefix = lists.prefix;
     const int tid = threadIdx.x, lane = tid & 63, b = a.b;
     // (shares that follow each other run on the same XCD, so that tiles of one prefix meet in its L2)
     const int share = (blockIdx.x & 7) * (a.shares >> 3) + (blockIdx.x >> 3), own_tiles = (a.group + kOwn - 1) / kOwn;
 
-    for (int i = tid; i <= b; i += 256) before[i] = 0;
+    for (int i = tid; i <= b; i += NT) before[i] = 0;
     __syncthreads();
     int bits = 0;
-    for (int s = tid; s < b; s += 256) {
+    for (int s = tid; s < b; s += NT) {
         int row, n, of = a.prefix_of[s], is = kLeftOut, steps = 0;
         bool too_long = false;
         if (paged_row(a.rows, s, row, n, too_long)) {
@@ -153,25 +180,25 @@ __global__ void __launch_bounds__(256, Elem<C>::kBytes * D == 512 && ROWS == 2 ?
     }
     if (bits && blockIdx.x == 0) atomicOr(a.status, bits);
     __syncthreads();
-    const int per = (b + 255) / 256, s0 = tid * per, s1 = s0 + per < b ? s0 + per : b;
+    const int per = (b + NT - 1) / NT, s0 = tid * per, s1 = s0 + per < b ? s0 + per : b;
     {
         int own = 0;
         for (int p = s0; p < s1; ++p) own += before[1 + p];
-        int at = sum_to(own, scratch) - own;
+        int at = sum_to(own, lists.scratch) - own;
         for (int p = s0; p < s1; ++p) {
             const int m = before[1 + p];
             members[p] = (uint16_t)at;
             at += m;
-            before[1 + p] = m ? steps_of(a.rows.cache_len[p]) * ((m * a.group + kTile - 1) / kTile) : 0;
+            before[1 + p] = m ? steps_of(a.rows.cache_len[p]) * ((m * a.group + TILE - 1) / TILE) : 0;
             if (p == b - 1) members[b] = (uint16_t)at;
         }
     }
     __syncthreads();
     {
-        const int each = (2 * b + 255) / 256, e0 = tid * each, e1 = e0 + each < 2 * b ? e0 + each : 2 * b;
+        const int each = (2 * b + NT - 1) / NT, e0 = tid * each, e1 = e0 + each < 2 * b ? e0 + each : 2 * b;
         int own = 0;
         for (int e = e0; e < e1; ++e) own += before[1 + e];
-        int at = sum_to(own, scratch) - own;
+        int at = sum_to(own, lists.scratch) - own;
         for (int e = e0; e < e1; ++e) {
             at += before[1 + e];
             before[1 + e] = at;
@@ -181,7 +208,7 @@ __global__ void __launch_bounds__(256, Elem<C>::kBytes * D == 512 && ROWS == 2 ?
     const int total = __builtin_amdgcn_readfirstlane(before[2 * b]) * a.h_kv;
     const PagedShares shares(total, a.shares);
     // what the join asks of this call: a wave has a sequence
-    for (int s = blockIdx.x * 4 + (tid >> 6); s < b; s += gridDim.x * 4) {
+    for (int s = blockIdx.x * WAVES + (tid >> 6); s < b; s += gridDim.x * WAVES) {
         const int is = prefix[s];
         int rank = 0;
         if (is != kNoPrefix && is != kLeftOut)
@@ -195,7 +222,7 @@ __global__ void __launch_bounds__(256, Elem<C>::kBytes * D == 512 && ROWS == 2 ?
                 to.members = members[is] - members[is - 1];
                 to.first = members[is - 1];
                 to.prefix_at = before[is - 1];
-                to.prefix_steps = (before[is] - before[is - 1]) / ((to.members * a.group + kTile - 1) / kTile);
+                to.prefix_steps = (before[is] - before[is - 1]) / ((to.members * a.group + TILE - 1) / TILE);
             }
             a.place[s] = to;
         }
@@ -218,46 +245,322 @@ __global__ void __launch_bounds__(256, Elem<C>::kBytes * D == 512 && ROWS == 2 ?
         const bool is_prefix = e < b;
         const int s = is_prefix ? e : e - b, at_member = __builtin_amdgcn_readfirstlane((int)members[is_prefix ? e : 0]),
                   count = is_prefix ? __builtin_amdgcn_readfirstlane((int)members[e + 1]) - at_member : 1;
-        const int columns = count * a.group, width = is_prefix ? kTile : kOwn, tiles = (columns + width - 1) / width, steps = of_head / tiles;
+        const int columns = count * a.group, width = is_prefix ? TILE : kOwn, tiles = (columns + width - 1) / width, steps = of_head / tiles;
         const int in_e = x - e_before * a.h_kv, unit = in_e / steps, kv = unit / tiles, tile = unit - kv * tiles, first = in_e - unit * steps;
-        const int last = steps - first < x1 - x ? steps : first + (x1 - x), n = a.rows.cache_len[s];
+        const int last = steps - first < x1 - x ? steps : first + (x1 - x), n = __builtin_amdgcn_readfirstlane(a.rows.cache_len[s]);
         const int begin = first * kPagedStep, end = last == steps ? n : last * kPagedStep, here = columns - tile * width < width ? columns - tile * width : width;
         const int64_t to = (int64_t)a.group * a.h_kv * (is_prefix ? at_member : b + s) + (int64_t)kv * columns + tile * width + (int64_t)share * kColumns;
         const int32_t* const table = a.block_table + (int64_t)s * a.max_pages;
-        auto emit = [&](int i, float all, float sum, const float (&y)[D / 16]) __attribute__((always_inline)) {
-            const int64_t at = to + i;
-            const int c = (tid & 15) * (D / 16);
-#pragma unroll
-            for (int z = 0; z < D / 16; z += 4) *reinterpret_cast<f32x4_t*>(a.part_out + at * D + c + z) = f32x4_t{y[z], y[z + 1], y[z + 2], y[z + 3]};
-            if (c == 0) *reinterpret_cast<float2*>(a.part_sum + at * 2) = float2{all, sum};
-        };
         if (is_prefix) {
             // rows of the sequences whose heads are columns of this tile
-            const int rank0 = tile * kTile / a.group, rank1 = (tile * kTile + here + a.group - 1) / a.group;
+            const int rank0 = tile * TILE / a.group, rank1 = (tile * TILE + here + a.group - 1) / a.group;
             int own = 0;
             for (int i = s0; i < s1; ++i) own += prefix[i] == e + 1;
-            int rank = sum_to(own, scratch) - own;
+            int rank = sum_to(own, lists.scratch) - own;
             for (int i = s0; i < s1; ++i)
                 if (prefix[i] == e + 1) {
                     if (rank >= rank0 && rank < rank1) member_row[rank - rank0] = a.rows.row_start ? a.rows.row_start[i + 1] - 1 : i;
                     ++rank;
                 }
             __syncthreads();
-            shared_part<T, C, D, ROWS>(a, table, kv, begin, end, here, part, tops, sums,
-                                       [&](int i) __attribute__((always_inline)) {
-                                           const int at = tile * kTile + i, rank = at / a.group;
-                                           return a.q + member_row[rank - rank0] * a.q_stride + ((int64_t)kv * a.group + at - rank * a.group) * (D * Elem<T>::kBytes);
-                                       },
-                                       emit);
+            prefix_part(table, kv, begin, end, here, [&](int i) __attribute__((always_inline)) {
+                const int at = tile * TILE + i, rank = at / a.group;
+                return a.q + member_row[rank - rank0] * a.q_stride + ((int64_t)kv * a.group + at - rank * a.group) * (D * Elem<T>::kBytes);
+            }, to);
         } else {
             const int row = a.rows.row_start ? a.rows.row_start[s + 1] - 1 : s;
             const char* const heads = a.q + row * a.q_stride + ((int64_t)kv * a.group + tile * kOwn) * (D * Elem<T>::kBytes);
-            shared_part<T, C, D, OWN>(a, table, kv, begin, end, here, part, tops, sums,
-                                      [&](int i) __attribute__((always_inline)) { return heads + (int64_t)i * (D * Elem<T>::kBytes); }, emit);
+            shared_part<T, C, D, OWN, WAVES>(a, table, kv, begin, end, here, lds, [&](int i) __attribute__((always_inline)) { return heads + (int64_t)i * (D * Elem<T>::kBytes); },
+                                             SharedEmit<D>{a.part_out, a.part_sum, to});
         }
         x += last - first;
         if (x == (e_before + of_head) * a.h_kv) ++e;
     }
+}
+
+// 16 ROWS columns to a prefix's unit: all types, pages of any size.
+template <typename T, typename C, int D, int ROWS, int OWN>
+__global__ void __launch_bounds__(256, Elem<C>::kBytes * D == 512 && ROWS == 2 ? 1 : 2) swa_paged_shared_kernel(SharedArgs a)
+{
+    __shared__ SharedLds<D, 4> lds;
+    __shared__ int scratch[4], member_row[16 * ROWS + 1];
+    extern __shared__ int lists[];
+    shared_share<T, C, D, 16 * ROWS, OWN, 4>(a, SharedLists(lists, a.b, scratch), member_row, lds,
+                                             [&](const int32_t* table, int kv, int begin, int end, int columns, auto from, int64_t to) __attribute__((always_inline)) {
+                                                 shared_part<T, C, D, ROWS, 4>(a, table, kv, begin, end, columns, lds, from, SharedEmit<D>{a.part_out, a.part_sum, to});
+                                             });
+}
+
+// ---- prefixes of many columns, 16 bit -------------------------------------------------------------------------------------------------------
+//
+// Bound by the matrix cores and the softmax's exponentials next to them.  Eight waves: four groups of 32 columns, and two halves of a unit's tokens, every other 32 of
+// them, whose results meet in LDS at its end (two workgroups of four waves would leave twice as many partial results).  As in swa_flash.hip a lane owns one column throughout: S^T = K Q^T
+// leaves lane l the logits of 16 keys for column l % 32, O^T = V^T P^T takes its weights as they lie; key and value tiles go from L2 straight to LDS, three buffers of them,
+// two tiles ahead, rows permuted by chunks instead of padded.  A wave stages eight tokens that follow each other, which lie in one page where page_size is a
+// multiple of eight: their place is a scalar, and the table's entry a scalar load, one tile ahead of its use.
+//
+// Weights are rounded once to the cache's type here (two numbers for a weight, as in the decode, are half as many products again, and 16-bit outputs come 16 to 21 %
+// nearer to the exact ones, whose own rounding both have).  In fp16 they are raised by 2^11: the largest is below 2^15, one of 2^-25 of it a normal number still.
+
+// The 16 weights of one lane's column, exp2(c scale - m), their sum, and the rescaling that goes with them: formed with the reference m as it is, and again where that turns out
+// too low (a sum above 2^15, or not finite, as on the first tile).
+template <typename T, int CT>
+__device__ __forceinline__ float column_weights(const float16_t& c, float scale, float& m, float& l, float16_t (&o)[CT], float (&p)[16])
+{
+    constexpr float kRaise = std::is_same_v<T, F16> ? 11.f : 0.f;
+    float sum;
+    auto weights = [&]() __attribute__((always_inline)) {
+        sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            p[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(c[i], scale, -m));
+            sum += p[i];
+        }
+    };
+    weights();
+    if (__any(sum > 32768.f)) {
+        float most = c[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) most = fmaxf(most, c[i]);
+        float lo, hi;
+        both_halves(most, lo, hi);
+        most = fmaxf(lo, hi) * scale - kRaise;
+        const float to = most > m ? most : m, down = __builtin_amdgcn_exp2f(m - to);
+        m = to;
+        l *= down;
+#pragma unroll
+        for (int t = 0; t < CT; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[t][i] *= down;
+        weights();
+    }
+    return sum;
+}
+
+constexpr int kWideColumns = 128;
+
+template <int D>
+constexpr int wide_tile_bytes() { return 32 * D * 2; }
+template <int D>
+constexpr int wide_lds_bytes() { return 12 * wide_tile_bytes<D>() > kWideColumns * (D + 6) * 4 ? 12 * wide_tile_bytes<D>() : kWideColumns * (D + 6) * 4; }
+
+// Tokens begin .. end - 1 (begin a multiple of 32) for up to 128 columns.
+template <typename T, int D, typename Q>
+__device__ __forceinline__ void wide_part(const SharedArgs& a, const int32_t* table_, int kv, int begin, int end, int columns, char* lds, Q from, int64_t to)
+{
+    constexpr int kRow = D * 2, kTile = wide_tile_bytes<D>(), NV = kRow / 32, CT = D / 32, kChunks = kRow / 16, kRowsPerLoad = 64 / kChunks, LD = 8 / kRowsPerLoad, PF = 2;
+    static_assert(2 * LD == NV / 2, "one load behind every second product of the first contraction");
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), group = wave & 3, half = wave >> 2, l32 = lane & 31, hb = lane >> 5;
+    char* const buf = lds + half * (6 * kTile);
+    char *const k0 = buf, *const v0 = buf + kTile, *const k1 = buf + 2 * kTile, *const v1 = buf + 3 * kTile, *const k2 = buf + 4 * kTile, *const v2 = buf + 5 * kTile;
+    const int rounds = (end - begin + 63) >> 6;
+    auto base_of = [&](int round) { return begin + round * 64 + half * 32; };
+
+    // The eight tokens that this wave stages of a round's tile (the last eight where there are none), and their page.
+    typedef const int32_t __attribute__((address_space(4))) * scalar_t;
+    const scalar_t table = (scalar_t)(uintptr_t)table_;
+    const int last8 = (end - 1) & ~7;
+    auto token_of = [&](int round) {
+        const int t = base_of(round) + group * 8;
+        return t < last8 ? t : last8;
+    };
+    auto page_of = [&](int t) { return (int)(((uint64_t)(uint32_t)t * a.page_mul) >> a.page_shift); };
+    auto swzK = [](int r) { return D == 128 ? (r & 15) : ((r >> 1) & 7); };
+    auto swzV = [](int r) { return D == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); };
+    uint32_t offK[LD], offV[LD];
+    auto offsets = [&](int last) {                       // rows past `last` of the eight read that one
+        int ln = lane;
+        asm volatile("" : "+v"(ln));                     // (computed where it is needed, not kept in registers around the loop)
+#pragma unroll
+        for (int x = 0; x < LD; ++x) {
+            const int j = x * kRowsPerLoad + ln / kChunks, r = j < last ? j : last, at = group * 8 + j;
+            offK[x] = (uint32_t)(r * kRow + (((ln % kChunks) ^ swzK(at)) << 4));
+            offV[x] = (uint32_t)(r * kRow + (((ln % kChunks) ^ swzV(at)) << 4));
+        }
+    };
+    int64_t at_row = 0;                                  // bytes before the eight rows in the pool
+    auto aim = [&](int round, int page) {
+        const int t = token_of(round);
+        at_row = ((int64_t)(page * a.h_kv + kv) * a.page_size + (t - page_of(t) * a.page_size)) * kRow;
+        if (base_of(round) + 32 > end) offsets(end - 1 - t);
+    };
+    auto load = [&](int x, char* dk, char* dv) {
+        if (x < LD) load_to_lds(a.pool.k_pages + at_row, offK[x], lds_address(dk) + (group * LD + x) * 1024);
+        else load_to_lds(a.pool.v_pages + at_row, offV[x - LD], lds_address(dv) + (group * LD + x - LD) * 1024);
+    };
+    offsets(8);
+    __syncthreads();                                     // (what was in LDS before has been read)
+    int page = table[page_of(token_of(0))], next_page = table[page_of(token_of(1))];
+    aim(0, page);
+#pragma unroll
+    for (int x = 0; x < 2 * LD; ++x) load(x, k0, v0);
+    Vec16 q[NV];
+    const int column = group * 32 + l32;
+    const char* const row = from(column < columns ? column : 0);
+#pragma unroll
+    for (int v = 0; v < NV; ++v) q[v] = load16(row + v * 32 + hb * 16);
+    // Fragment addresses, as in swa_flash.hip: key fragment v is row l32, chunk 2 v + hb; value fragment (ct, v) keys 16 v + 4 hb + 0..3 and 16 v + 8 + 4 hb + 0..3 of channel
+    // 32 ct + l32.
+    const uint32_t ka = (uint32_t)(l32 * kRow + ((hb ^ swzK(l32)) << 4));
+    const int j16 = lane & 15;
+    const uint32_t va = (uint32_t)((4 * hb + (j16 >> 2)) * kRow + (((2 * ((lane >> 4) & 1) + ((j16 & 3) >> 1)) ^ swzV(j16 >> 2)) << 4) + (j16 & 1) * 8);
+    // (the queries are waited for here, where the compiler sees it, and not with the tiles requested since in every round)
+    __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0)
+    if (rounds > 1) {
+        page = next_page;
+        next_page = table[page_of(token_of(2))];
+        aim(1, page);
+#pragma unroll
+        for (int x = 0; x < 2 * LD; ++x) load(x, k1, v1);
+    }
+
+    float16_t o[CT];
+#pragma unroll
+    for (int t = 0; t < CT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+    float m = -3.0e38f, l = 0.f;                         // (finite, so that logits of -inf weigh nothing before the first finite one too)
+    const bool mine = group * 32 < columns;
+
+    // tail: the round's tile may end inside; more: the tile two rounds on is requested
+    auto compute = [&](bool tail, bool more, int round, const char* sk, const char* sv, char* nk, char* nv) __attribute__((always_inline)) {
+        if (more) {
+            aim(round + 2, next_page);
+            next_page = table[page_of(token_of(round + 3))];
+        }
+        if (!mine) {
+            if (more)
+#pragma unroll
+                for (int x = 0; x < 2 * LD; ++x) load(x, nk, nv);
+            return;
+        }
+        float16_t c;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) c[i] = 0.f;
+        auto kfrag = [&](int v) { return load16(sk + (ka ^ (v << 5))); };
+        Vec16 kf[NV];
+#pragma unroll
+        for (int v = 0; v < PF && v < NV; ++v) kf[v] = kfrag(v);
+#pragma unroll
+        for (int v = 0; v < NV; ++v) {
+            if (v + PF < NV) kf[v + PF] = kfrag(v + PF);
+            __builtin_amdgcn_sched_barrier(0);
+            c = Mfma<T>::run(kf[v], q[v], c);
+            __builtin_amdgcn_sched_barrier(0);
+            if ((v & 1) && more) load(v >> 1, nk, nv);
+        }
+        if (tail) {
+            const int left = end - base_of(round);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) c[i] = 8 * (i / 4) + 4 * hb + (i % 4) < left ? c[i] : -INFINITY;
+        }
+        float p[16];
+        const float sum = column_weights<T>(c, a.pool.scale, m, l, o, p);
+        l += sum;
+        const Vec16 pv[2] = {pack<T>(p), pack<T>(p + 8)};
+        auto vfrag = [&](int f) {
+            const char* const at = sv + ((va ^ (f % CT << 6)) + f / CT * 16 * kRow);
+            return lds_read_tr(at, at + 8 * kRow);
+        };
+        Vec16 vf[2 * CT];
+#pragma unroll
+        for (int f = 0; f < PF && f < 2 * CT; ++f) vf[f] = vfrag(f);
+#pragma unroll
+        for (int f = 0; f < 2 * CT; ++f) {
+            if (f + PF < 2 * CT) vf[f + PF] = vfrag(f + PF);
+            __builtin_amdgcn_sched_barrier(0);
+            o[f % CT] = Mfma<T>::run(vf[f], pv[f / CT], o[f % CT]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // A round's tiles are read while the next two are on their way; loads return in order, so "all but the newest tile's" is a count.
+    auto ready = [&](bool newer) {
+        if (newer) __builtin_amdgcn_s_waitcnt(0x0070 | (2 * LD));      // vmcnt(2 LD) lgkmcnt(0)
+        else __builtin_amdgcn_s_waitcnt(0x0070);                       // vmcnt(0) lgkmcnt(0)
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    int round = 0;
+    for (; round + 4 < rounds; round += 3) {
+        ready(true);
+        compute(false, true, round, k0, v0, k2, v2);
+        ready(true);
+        compute(false, true, round + 1, k1, v1, k0, v0);
+        ready(true);
+        compute(false, true, round + 2, k2, v2, k1, v1);
+    }
+    // one to four are left, of which the very last may end inside its tiles: the values behind its tokens are zeros then (a weight of 0 times what is no number is none)
+    for (int i = 0; round < rounds; ++round, i = i == 2 ? 0 : i + 1) {
+        char *const sk = i == 0 ? k0 : i == 1 ? k1 : k2, *const sv = i == 0 ? v0 : i == 1 ? v1 : v2, *const nk = i == 0 ? k2 : i == 1 ? k0 : k1,
+                    *const nv = i == 0 ? v2 : i == 1 ? v0 : v1;
+        ready(round + 1 < rounds);
+        if (round + 1 == rounds && begin + rounds * 64 > end) {
+            const int left = end - base_of(round) < 0 ? 0 : end - base_of(round);
+            for (int x = (tid & 255) * 16 + left * kRow; x < kTile; x += 4096) store16(sv + x, Vec16{0u, 0u, 0u, 0u});
+            __syncthreads();
+        }
+        compute(true, round + 2 < rounds, round, sk, sv, nk, nv);
+    }
+    float lo, hi;
+    both_halves(l, lo, hi);
+    l = lo + hi;
+    __syncthreads();
+
+    // The second half's results to the first's, and from there to memory, whole rows at a time.
+    constexpr int kPitch = D + 4;
+    float* const result = reinterpret_cast<float*>(lds);
+    float* const stats = result + kWideColumns * kPitch;
+    if (half == 1 && mine) {
+#pragma unroll
+        for (int t = 0; t < CT; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g)
+                *reinterpret_cast<f32x4_t*>(result + column * kPitch + 32 * t + 8 * g + 4 * hb) = f32x4_t{o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]};
+        if (hb == 0) *reinterpret_cast<float2*>(stats + 2 * column) = float2{m, l};
+    }
+    __syncthreads();
+    if (half == 0 && mine) {
+        const float2 other = *reinterpret_cast<const float2*>(stats + 2 * column);
+        const float top = fmaxf(m, other.x), here = __builtin_amdgcn_exp2f(m - top), there = __builtin_amdgcn_exp2f(other.x - top);
+#pragma unroll
+        for (int t = 0; t < CT; ++t)
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                f32x4_t* const at = reinterpret_cast<f32x4_t*>(result + column * kPitch + 32 * t + 8 * g + 4 * hb);
+                *at = f32x4_t{o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]} * here + *at * there;
+            }
+        if (hb == 0 && column < columns) *reinterpret_cast<float2*>(a.part_sum + (to + column) * 2) = float2{top, l * here + other.y * there};
+    }
+    __syncthreads();
+    for (int i = tid; i < columns * (D / 4); i += 512) {
+        const int r = i / (D / 4), c = i % (D / 4) * 4;
+        *reinterpret_cast<f32x4_t*>(a.part_out + (to + r) * D + c) = *reinterpret_cast<const f32x4_t*>(result + r * kPitch + c);
+    }
+}
+
+// (sequences' own tokens sixteen columns at a time: thirty-two would not fit the registers beside the rest)
+template <typename T, int D>
+__global__ void __launch_bounds__(512, 2) swa_paged_shared_wide_kernel(SharedArgs a)
+{
+    extern __shared__ __align__(16) char lds[];          // tiles, then the lists
+    __shared__ int scratch[8], member_row[kWideColumns + 1];
+    SharedLds<D, 8>& sums = *reinterpret_cast<SharedLds<D, 8>*>(lds);
+    static_assert(sizeof(SharedLds<D, 8>) <= wide_lds_bytes<D>(), "in the tiles' place");
+    shared_share<T, T, D, kWideColumns, 1, 8>(
+        a, SharedLists(reinterpret_cast<int*>(lds + wide_lds_bytes<D>()), a.b, scratch), member_row, sums,
+        [&](const int32_t* table, int kv, int begin, int end, int columns, auto from, int64_t to) __attribute__((always_inline)) {
+            // (a page outside the pool is left out of the sums, which the other form of the work looks after)
+            bool bad = false;
+            for (int i = begin / a.page_size + (int)threadIdx.x; i <= (end - 1) / a.page_size; i += 512) bad |= (uint32_t)table[i] >= (uint32_t)a.n_pages;
+            if (!__syncthreads_or(bad)) {
+                wide_part<T, D>(a, table, kv, begin, end, columns, lds, from, to);
+            } else {
+                for (int c = 0; c < columns; c += 16)
+                    shared_part<T, T, D, 1, 8>(a, table, kv, begin, end, columns - c < 16 ? columns - c : 16, sums, [&](int i) __attribute__((always_inline)) { return from(c + i); },
+                                               SharedEmit<D>{a.part_out, a.part_sum, to + c});
+            }
+        });
 }
 
 // A query head's partial results, the prefix's and its own, to its output.
@@ -290,13 +593,20 @@ __global__ void __launch_bounds__(256) swa_paged_join_shared_kernel(SharedArgs a
                             count[0] + count[1], a.out, a.lse, (int64_t)at.row * a.h_q + hq);
 }
 
-constexpr int kSharedShares = 512;                 // two workgroups to a CU
-constexpr size_t kSharedOwnLds = 36 * 1024;        // of the kernel, at most, beside the lists
+// Columns that a prefix can have.
+static int64_t most_columns(const swa_paged_params& p) { return (int64_t)(p.b - 1) * (p.h_q / p.h_kv); }
 
-// Sixteens of columns of a prefix's unit.
-static int shared_rows(const swa_paged_params& p) { return (int64_t)(p.b - 1) * (p.h_q / p.h_kv) <= 16 ? 1 : 2; }
+// Columns of a prefix's unit, in sixteens.  More than 32 go to the wide form where it serves them.
+static int shared_rows(const swa_paged_params& p)
+{
+    const int64_t most = most_columns(p);
+    return most <= 16 ? 1 : most <= 32 || p.dtype == SWA_F32 || paged_int8(p) || p.page_size % 8 != 0 ? 2 : kWideColumns / 16;
+}
 
-static int64_t shared_columns(const swa_paged_params& p) { return 2 * (int64_t)p.b * p.h_q + (int64_t)kSharedShares * 32; }
+static int shared_shares(int rows) { return rows > 2 ? 256 : 512; }    // a workgroup to a CU, or two
+
+// (whatever page_size a call states)
+static int64_t shared_columns(const swa_paged_params& p) { return 2 * (int64_t)p.b * p.h_q + (most_columns(p) > 32 ? 256 * kWideColumns : 512 * 32); }
 
 size_t paged_shared_bytes(const swa_paged_params& p)
 {
@@ -306,14 +616,23 @@ size_t paged_shared_bytes(const swa_paged_params& p)
 template <typename T, typename C, int D>
 static int launch_shared_form(const SharedArgs& a, int rows, int own, hipStream_t stream)
 {
-    auto kernel = rows == 1 ? (own == 1 ? swa_paged_shared_kernel<T, C, D, 1, 1> : swa_paged_shared_kernel<T, C, D, 1, 2>)
-                            : (own == 1 ? swa_paged_shared_kernel<T, C, D, 2, 1> : swa_paged_shared_kernel<T, C, D, 2, 2>);
-    const size_t lds = sizeof(int) * (2 * (size_t)a.b + 1) + sizeof(uint16_t) * (2 * (size_t)a.b + 1) + 2;
-    if (lds + kSharedOwnLds > 64 * 1024) {
+    void (*kernel)(SharedArgs) = rows == 1 ? (own == 1 ? swa_paged_shared_kernel<T, C, D, 1, 1> : swa_paged_shared_kernel<T, C, D, 1, 2>)
+                                           : (own == 1 ? swa_paged_shared_kernel<T, C, D, 2, 1> : swa_paged_shared_kernel<T, C, D, 2, 2>);
+    size_t lds = shared_lists_bytes(a.b), of_its_own = 36 * 1024;
+    int threads = 256;
+    if constexpr (std::is_same_v<T, C> && !std::is_same_v<T, F32>) {
+        if (rows > 2) {
+            kernel = swa_paged_shared_wide_kernel<T, D>;
+            lds += wide_lds_bytes<D>();
+            of_its_own = 1024;
+            threads = 512;
+        }
+    }
+    if (lds + of_its_own > 64 * 1024) {
         const int rc = ensure_dynamic_lds(reinterpret_cast<const void*>(kernel), lds > 49 * 1024 ? lds : 49 * 1024);
         if (rc != SWA_OK) return rc;
     }
-    launch_kernel(kernel, dim3((unsigned)a.shares), dim3(256), lds, stream, a);
+    launch_kernel(kernel, dim3((unsigned)a.shares), dim3(threads), lds, stream, a);
     launch_kernel(swa_paged_join_shared_kernel<T, D>, dim3((unsigned)(a.b * a.h_q)), dim3(256), 0, stream, a, 16 * rows, 16 * own);
     return SWA_OK;
 }
@@ -343,10 +662,10 @@ int launch_paged_shared(const swa_paged_params& p, const swa_rows& q, int32_t n_
     a.n_pages = p.n_pages;
     a.max_pages = p.max_pages;
     a.group = p.h_q / p.h_kv;
-    a.shares = kSharedShares;
     page_divisor(p.page_size, a.page_mul, a.page_shift);
     a.sixteens = p.page_size % 16 == 0;
-    const int rows = shared_rows(p), own = a.group > 16 ? 2 : 1;
+    const int rows = shared_rows(p), own = rows <= 2 && a.group > 16 ? 2 : 1;
+    a.shares = shared_shares(rows);
     // (steps are 32-bit numbers: of every sequence's own tokens, and of as many prefixes as may be)
     const int64_t tiles = (int64_t)p.b * ((a.group + 16 * own - 1) / (16 * own)) + ((int64_t)p.b * a.group + 16 * rows - 1) / (16 * rows) + p.b;
     if (tiles * p.h_kv > 0x7fffffffLL / ((a.rows.len_max + kPagedStep - 1) / kPagedStep) || (uint64_t)p.b * p.h_q * 256 > 0xffffffffULL) return SWA_ERR_CAPACITY;

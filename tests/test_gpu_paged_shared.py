@@ -79,6 +79,8 @@ def check_shared(B, lens, prefix_of, h_q, h_kv, d, dtype, page, int8=False, scal
         if int8:
             steps = (2.0 ** -16, 0.0)                        # (codes are exact in either type, and queries are multiplied as they are)
         want, want_lse, tol, lse_tol = R.attention(q[row].double(), kr, vr, scale or d ** -0.5, dtype, *steps)
+        nothing = want_lse == -math.inf                      # every logit is -inf: out = 0
+        want[nothing], tol[nothing], lse_tol[nothing] = 0, 0, 0
         for name, x, y, z in (("out", got[row], want, tol),) + ((("lse", got_lse[row], want_lse, lse_tol),) if lse else ()):
             fine = torch.isfinite(y)
             assert torch.equal(torch.isnan(x), torch.isnan(y)) and torch.equal(x[~fine & ~torch.isnan(y)], y[~fine & ~torch.isnan(y)]), (name, s)
@@ -122,6 +124,47 @@ def test_long_prefixes_are_split_and_joined(B, dtype, int8):
     check_shared(B, [20011, 5, 300, 2000], behind(1, [0, 0, 0]), 4, 1, 128, t, 16, int8=int8)
     check_shared(B, [9000, 3001, 5, 0, 300, 2000], behind(2, [0, 1, 0, 1]), 8, 2, 64, t, 64, int8=int8, len_bound=9000)
     check_shared(B, [5000] + [20] * 40, behind(1, [0] * 40), 16, 2, 64, t, 16, int8=int8)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("page", [8, 16, 24, 256])
+def test_many_columns(B, dtype, d, page):
+    """More than 32 query heads behind a prefix: whole and part tiles of columns, of tokens and of rounds."""
+    t = TYPES[dtype]
+    for n in (1, 31, 32, 33, 64, 65, 100, 127, 128, 129, 192, 193, 255, 257, 320, 450, 1000):
+        check_shared(B, [n] + [5, 0, 40, 17, 1] * 2, behind(1, [0] * 10), 8, 2, d, t, page)
+    for members, h_q, h_kv in ((33, 1, 1), (11, 12, 4), (9, 16, 1), (8, 20, 1), (33, 8, 2), (3, 40, 1), (2, 33, 1), (3, 66, 2)):
+        check_shared(B, [500, 129] + [i % 19 for i in range(2 * members)], behind(2, [0, 1] * members), h_q, h_kv, d, t, page)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_many_columns_over_long_prefixes(B, dtype):
+    t = TYPES[dtype]
+    check_shared(B, [30011] + [30] * 20, behind(1, [0] * 20), 8, 1, 128, t, 16, len_bound=30011)
+    check_shared(B, [9001, 2500] + [30] * 40, behind(2, [0, 1] * 20), 8, 2, 64, t, 64)
+    for loud in (0.1, 5.0, 20.0):
+        check_shared(B, [3000] + [30] * 20, behind(1, [0] * 20), 8, 1, 128, t, 16, loud=loud)
+
+
+def test_many_columns_and_what_is_reported_or_not_finite(B):
+    lens, own = [300] + [i * 7 % 40 for i in range(24)], behind(1, [0] * 24)
+    for t in (torch.float16, torch.bfloat16):
+        for d in (64, 128):
+            check_shared(B, lens, own, 4, 2, d, t, 16, bad=[(0, 3, -1), (0, 9, 10 ** 6), (3, 0, 2 ** 31 - 1)])
+
+        def edit(k, v, q, table):
+            v[table[0, 2], 0, 3, 5], v[table[0, 18], 1, 11, 7] = math.inf, -math.inf
+            q[7, 3, 1], k[table[5, 0], 0, 0, 2] = math.nan, math.nan
+        check_shared(B, lens, own, 4, 2, 64, t, 16, edit=edit)
+
+        def cold(k, v, q, table):
+            q[:] = 0
+            k[:, :, :, 0] = -math.inf                        # every logit is -inf
+            q[:, :, 0] = 1
+        check_shared(B, [300] + [0] * 24, own, 4, 2, 64, t, 16, edit=cold)
+        starts = [0, 0] + list(range(1, 25))
+        check_shared(B, lens, own, 4, 2, 128, t, 16, row_start=starts, n_rows=24, slot=[i % 5 - 1 for i in range(24)], strided=True)
 
 
 def test_many_prefixes_and_many_sequences(B):
