@@ -156,18 +156,20 @@ __global__ void __launch_bounds__(64 * WAVES, Elem<C>::kBytes * D == 512 || (ROW
     });
 }
 
-// The chunks of a list and query head to its output, in their order.
-template <typename T, int D>
+// The chunks of a list and query head to its output.
+template <typename T, int D, int WAVES>
 __global__ void __launch_bounds__(256) swa_paged_join_selected_kernel(SelectedArgs a)
 {
-    const int s = blockIdx.x / a.h_q, hq = blockIdx.x - s * a.h_q, kv = hq / a.group, of = hq - kv * a.group, pair = s * a.h_kv + kv;
+    const int at = blockIdx.x * (4 / WAVES) + (WAVES == 1 ? threadIdx.x >> 6 : 0);
+    if (at >= a.b * a.h_q) return;
+    const int s = at / a.h_q, hq = at - s * a.h_q, kv = hq / a.group, of = hq - kv * a.group, pair = s * a.h_kv + kv;
     int row, n;
     bool too_long = false, bad = false;
     if (!paged_row(a.rows, s, row, n, too_long)) return;
     const int tokens = selected_count(a, pair, bad) * a.page_size;
     if (tokens <= a.chunk) return;
     const int64_t stride = a.row_tiles * a.heads, first = pair * a.ranges * stride + of / a.tile_heads * a.heads + of % a.tile_heads;
-    paged_join_pieces<T, D>(a.part_out, a.part_sum, [&](int i) __attribute__((always_inline)) { return first + i * stride; }, (tokens + a.chunk - 1) / a.chunk, a.out, a.lse,
+    paged_join_pieces<T, D, WAVES>(a.part_out, a.part_sum, [&](int i) __attribute__((always_inline)) { return first + i * stride; }, (tokens + a.chunk - 1) / a.chunk, a.out, a.lse,
                             (int64_t)row * a.h_q + hq);
 }
 
@@ -182,7 +184,11 @@ static int launch_selected_form(const SelectedArgs& a, int span, hipStream_t str
     auto kernel = single ? (one ? swa_paged_selected_kernel<T, C, D, 1, 1> : swa_paged_selected_kernel<T, C, D, 2, 1>)
                          : (one ? swa_paged_selected_kernel<T, C, D, 1, 4> : swa_paged_selected_kernel<T, C, D, 2, 4>);
     launch_kernel(kernel, dim3((unsigned)groups), dim3(single ? 64 : 256), 0, stream, a);
-    if (a.ranges > 1) launch_kernel(swa_paged_join_selected_kernel<T, D>, dim3((unsigned)(a.b * a.h_q)), dim3(256), 0, stream, a);
+    if (a.ranges > 1) {
+        const unsigned rows = (unsigned)(a.b * a.h_q);
+        if (rows >= 1024) launch_kernel(swa_paged_join_selected_kernel<T, D, 1>, dim3((rows + 3) / 4), dim3(256), 0, stream, a);
+        else launch_kernel(swa_paged_join_selected_kernel<T, D, 4>, dim3(rows), dim3(256), 0, stream, a);
+    }
     return SWA_OK;
 }
 

@@ -1,11 +1,13 @@
 // Attention of one new token per sequence over a prefix that several sequences share, and over each one's own pages.
 //
-// A prefix's keys and values are read for all of its sequences at once: their query heads are the columns of its products, 16 ROWS of them to a workgroup.  The call's
-// work is prefixes, then sequences, each by key head and tile of columns, in steps of 128 tokens; laid end to end it is cut into as many equal shares as there are
-// workgroups, whatever the lengths and the numbers of sequences are.  Every workgroup sums it up by itself.  A share's part of a unit (one prefix or sequence, key head
-// and tile) is a partial result of each of its columns; a second launch joins the prefix's and the sequence's own ones in their order.
-//   Partial results: unit u's column i from share g lies at R_u + 16 ROWS g + i, with R_u the columns of the units before it: units and shares follow each
-//   other in the same order, and a share that ends one unit begins the next behind that one's columns, so no two of them meet.
+// A prefix's keys and values are read for all of its sequences at once: their query heads are the columns of its products.  Units of work are a prefix, key head and tile of
+// columns, and a sequence, key head and up to 16 of its query heads.  The prefixes' units, in steps of 128 tokens, are laid end to end and cut into as many equal shares as there
+// are workgroups, and the sequences', in steps of 32, into as many as there are waves, whatever the lengths and the numbers of sequences are; every workgroup sums both up by
+// itself.  So each has as much of either as the others, and a wave has a short sequence to itself, with no other wave to wait for (as units of eight waves they took 5 us each: 64
+// sequences of 1 to 300 tokens behind 32768, 64 query and 8 key heads, 177 us on the last workgroups, 89 on the others).
+//   A share's part of a unit is a partial result of each of its columns; a second launch joins the prefix's and the sequence's own ones in their order.  Unit u's column i
+// from share g lies at R_u + W g + i, with R_u the columns of the units before it and W the columns of a unit at most: units and shares follow each other in the same order, and a
+// share that ends one unit begins the next behind that one's columns, so no two of them meet.
 #include "swa_paged_tile.hpp"
 
 namespace swa {
@@ -15,7 +17,7 @@ struct alignas(16) SharedPlace {
     int32_t row, rank;                             // its row, and its number among the prefix's sequences
     int32_t members, prefix_at, prefix_steps;      // those, the prefix's first step (of one key head, like `at`), the steps of a unit
     int32_t first;                                 // sequences of the prefixes before
-    int32_t at, steps;                             // of the sequence itself
+    int32_t at, steps;                             // of the sequence itself, likewise
 };
 
 struct SharedArgs {
@@ -27,10 +29,11 @@ struct SharedArgs {
     char* out;
     float* lse;
     float *part_out, *part_sum;                    // [columns, D] and [.., 2] (maximum, sum)
-    SharedPlace* place;                            // [b], and behind them the steps of the call
+    SharedPlace* place;                            // [b], and behind them the steps of all prefixes, and of all sequences
     int32_t* status;
     int32_t b, h_q, h_kv, page_size, n_pages, max_pages;
-    int32_t group, shares;
+    int32_t group, shares;                         // workgroups
+    int64_t own_columns;                           // partial results of the prefixes, before those of the sequences
     uint32_t page_mul;                             // t / page_size = t * page_mul >> page_shift for 0 <= t < 2^31
     int32_t page_shift;
     int32_t sixteens;                              // pages are whole sixteens of tokens
@@ -39,6 +42,10 @@ struct SharedArgs {
 constexpr int kNoPrefix = 0, kLeftOut = 0xffff;    // of a sequence, where it has no prefix or the call leaves it out; else the prefix's number and 1
 
 __device__ __forceinline__ int steps_of(int tokens) { return (tokens + kPagedStep - 1) / kPagedStep; }
+
+// A sequence's own tokens: steps of 32, and one that stands for what a unit costs before its first key.
+constexpr int kOwnStep = 32, kOwnColumns = 16;
+__device__ __forceinline__ int own_steps_of(int tokens) { return tokens > 0 ? 1 + (tokens + kOwnStep - 1) / kOwnStep : 0; }
 
 // A partial result, by sixteen threads.
 template <int D>
@@ -135,28 +142,86 @@ __device__ __forceinline__ void shared_part(const SharedArgs& a, const int32_t* 
     paged_join_waves<T, C, D, ROWS, WAVES>(lds.part, lds.tops, lds.sums, top, sum, acc, columns, who, emit);
 }
 
+// Tokens begin .. end - 1 of a sequence by one wave, for up to 16 query heads, which begin at `from`.
+template <typename T, typename C, int D>
+__device__ __forceinline__ void own_part(const SharedArgs& a, const int32_t* table, int kv, int begin, int end, int columns, const char* from, int64_t to)
+{
+    typedef PagedTile<T, C, D, 1> S;
+    constexpr int kKeys = S::kKeys, kSteps = S::kSteps, kChannels = S::kChannels;
+    const int lane = threadIdx.x & 63, col = lane & 15, j = lane >> 4;
+    Vec16 q[1][kSteps];
+    const char* const at = from + (col < columns ? col : 0) * (D * Elem<T>::kBytes);
+#pragma unroll
+    for (int c = 0; c < kSteps; ++c) q[0][c] = load16(at + S::query_at(c, j));
+    float top[1] = {-INFINITY}, sum[1] = {0.f};
+    f32x4_t acc[1][kChannels];
+#pragma unroll
+    for (int e = 0; e < kChannels; ++e) acc[0][e] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    bool bad = false;
+    auto page_of = [&](int base) {
+        const int t = base + (lane & (kKeys - 1));
+        return (int)(((uint64_t)(uint32_t)(t < end ? t : end - 1) * a.page_mul) >> a.page_shift);
+    };
+    auto row_of = [&](int base, int page) {
+        const int t = base + (lane & (kKeys - 1));
+        const bool live = t < end, in_pool = (uint32_t)page < (uint32_t)a.n_pages;
+        bad |= live && !in_pool;
+        return live && in_pool ? (page * a.h_kv + kv) * a.page_size + t - page_of(base) * a.page_size : -1;
+    };
+    int next = begin, page = table[page_of(next)];
+    while (next < end) {
+        const int rows = row_of(next, page);
+        next += kKeys;
+        if (next < end) page = table[page_of(next)];
+        if (a.sixteens && !__any(rows < 0)) paged_take<T, C, D, 1, true>(a.pool, rows, q, top, sum, acc);
+        else paged_take<T, C, D, 1, false>(a.pool, rows, q, top, sum, acc);
+    }
+    if (bad) atomicOr(a.status, kStatusBadRequestBit);
+    sum[0] += __shfl_xor(sum[0], 16, 64);
+    sum[0] += __shfl_xor(sum[0], 32, 64);
+    if (col < columns) {
+        float* const out = a.part_out + (to + col) * D;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < kChannels; e += 4)
+                *reinterpret_cast<f32x4_t*>(out + (S::kWide ? (e / 4) * 64 + (4 * j + i) * 4 : (4 * j + i) * kChannels + e)) = f32x4_t{acc[0][e][i], acc[0][e + 1][i], acc[0][e + 2][i], acc[0][e + 3][i]};
+        if (j == 0) *reinterpret_cast<float2*>(a.part_sum + (to + col) * 2) = float2{top[0] - S::kRaise, sum[0]};
+    }
+}
+
 // What every workgroup sums up by itself, in LDS.
 struct SharedLists {
-    int* before;                                         // [2 b + 1]: steps of a key head before prefix e, and before sequence e - b
+    int *before, *own;                                   // [b + 1]: steps of a key head before prefix p, and before sequence s
     uint16_t *members, *prefix;                          // [b + 1]: sequences of the prefixes before; [b]: a sequence's own prefix
-    int* scratch;                                        // one for each wave
-    __device__ __forceinline__ SharedLists(int* lds, int b, int* scratch_) : before(lds), members(reinterpret_cast<uint16_t*>(lds + 2 * b + 1)), prefix(members + b + 1), scratch(scratch_) {}
+    int* scratch;                                        // three for each wave
+    __device__ __forceinline__ SharedLists(int* lds, int b, int* scratch_) : before(lds), own(lds + b + 1), members(reinterpret_cast<uint16_t*>(own + b + 1)), prefix(members + b + 1), scratch(scratch_) {}
 };
-constexpr size_t shared_lists_bytes(int64_t b) { return (sizeof(int) * (2 * b + 1) + sizeof(uint16_t) * (2 * b + 1) + 15) / 16 * 16; }
+constexpr size_t shared_lists_bytes(int64_t b) { return (sizeof(int) * (2 * b + 2) + sizeof(uint16_t) * (2 * b + 1) + 15) / 16 * 16; }
 
-// The lists, what the join asks of this call, and then this workgroup's share, prefixes by prefix_part and sequences by shared_part.
-//   TILE, OWN: columns of a unit of a prefix's tokens, sixteens of them in one of a sequence's own.
-template <typename T, typename C, int D, int TILE, int OWN, int WAVES, typename P>
-__device__ __forceinline__ void shared_share(const SharedArgs& a, const SharedLists& lists, int (&member_row)[TILE + 1], SharedLds<D, WAVES>& lds, P prefix_part)
+// The unit of step x: its entry in a list of steps before entries (0 .. b), of which each has h_kv times as many.
+__device__ __forceinline__ int entry_of(const int* before, int b, int h_kv, int x)
 {
-    constexpr int kOwn = 16 * OWN, kColumns = TILE > kOwn ? TILE : kOwn, NT = 64 * WAVES;
-    int* const before = lists.before;
+    int e = 0;
+    for (int above = b; e + 1 < above;) {
+        const int mid = (e + above) >> 1;
+        if (before[mid] * h_kv <= x) e = mid; else above = mid;
+    }
+    return __builtin_amdgcn_readfirstlane(e);
+}
+
+// The lists, what the join asks of this call, and then this workgroup's shares: prefixes' units of TILE columns by prefix_part, and sequences.
+template <typename T, typename C, int D, int TILE, int WAVES, typename P>
+__device__ __forceinline__ void shared_share(const SharedArgs& a, const SharedLists& lists, int (&member_row)[TILE + 1], P prefix_part)
+{
+    constexpr int NT = 64 * WAVES;
+    int *const before = lists.before, *const own = lists.own;
     uint16_t *const members = lists.members, *const prefix = lists.prefix;
-    const int tid = threadIdx.x, lane = tid & 63, b = a.b;
-    // (shares that follow each other run on the same XCD, so that tiles of one prefix meet in its L2)
-    const int share = (blockIdx.x & 7) * (a.shares >> 3) + (blockIdx.x >> 3), own_tiles = (a.group + kOwn - 1) / kOwn;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = a.b;
+    const int own_tiles = (a.group + kOwnColumns - 1) / kOwnColumns;
 
     for (int i = tid; i <= b; i += NT) before[i] = 0;
+    if (tid == 0) own[0] = 0;
     __syncthreads();
     int bits = 0;
     for (int s = tid; s < b; s += NT) {
@@ -171,44 +236,40 @@ __device__ __forceinline__ void shared_share(const SharedArgs& a, const SharedLi
                 else if (m > a.rows.len_max) bits |= kStatusCapacityBit;
                 is = m < 0 || m > a.rows.len_max ? kLeftOut : of + 1;
             }
-            if (is != kLeftOut) steps = steps_of(n) * own_tiles;
+            if (is != kLeftOut) steps = own_steps_of(n) * own_tiles;
             if (is != kLeftOut && is != kNoPrefix) atomicAdd(&before[1 + of], 1);
         }
         if (too_long) bits |= kStatusCapacityBit;
         prefix[s] = (uint16_t)is;
-        before[1 + b + s] = steps;
+        own[1 + s] = steps;
     }
     if (bits && blockIdx.x == 0) atomicOr(a.status, bits);
     __syncthreads();
+    // running sums, over `per` entries that follow each other a thread
     const int per = (b + NT - 1) / NT, s0 = tid * per, s1 = s0 + per < b ? s0 + per : b;
-    {
-        int own = 0;
-        for (int p = s0; p < s1; ++p) own += before[1 + p];
-        int at = sum_to(own, lists.scratch) - own;
-        for (int p = s0; p < s1; ++p) {
-            const int m = before[1 + p];
-            members[p] = (uint16_t)at;
-            at += m;
-            before[1 + p] = m ? steps_of(a.rows.cache_len[p]) * ((m * a.group + TILE - 1) / TILE) : 0;
-            if (p == b - 1) members[b] = (uint16_t)at;
-        }
+    int sums[3] = {0, 0, 0};                             // sequences behind prefixes, those's steps, own steps
+    for (int p = s0; p < s1; ++p) {
+        const int m = before[1 + p];
+        sums[0] += m;
+        sums[1] += m ? steps_of(a.rows.cache_len[p]) * ((m * a.group + TILE - 1) / TILE) : 0;
+        sums[2] += own[1 + p];
+        members[p + 1] = (uint16_t)sums[0];
+        before[1 + p] = sums[1];
+        own[1 + p] = sums[2];
     }
-    __syncthreads();
-    {
-        const int each = (2 * b + NT - 1) / NT, e0 = tid * each, e1 = e0 + each < 2 * b ? e0 + each : 2 * b;
-        int own = 0;
-        for (int e = e0; e < e1; ++e) own += before[1 + e];
-        int at = sum_to(own, lists.scratch) - own;
-        for (int e = e0; e < e1; ++e) {
-            at += before[1 + e];
-            before[1 + e] = at;
-        }
+    const int here[3] = {sums[0], sums[1], sums[2]};
+    sums_to(sums, lists.scratch);
+    for (int p = s0; p < s1; ++p) {
+        members[p + 1] = (uint16_t)(members[p + 1] + sums[0] - here[0]);
+        before[1 + p] += sums[1] - here[1];
+        own[1 + p] += sums[2] - here[2];
     }
+    if (tid == 0) members[0] = 0;
     __syncthreads();
-    const int total = __builtin_amdgcn_readfirstlane(before[2 * b]) * a.h_kv;
-    const PagedShares shares(total, a.shares);
+    const int total = __builtin_amdgcn_readfirstlane(before[b]) * a.h_kv, own_total = __builtin_amdgcn_readfirstlane(own[b]) * a.h_kv;
+    const PagedShares shares(total, a.shares), own_shares(own_total, a.shares * WAVES);
     // what the join asks of this call: a wave has a sequence
-    for (int s = blockIdx.x * WAVES + (tid >> 6); s < b; s += gridDim.x * WAVES) {
+    for (int s = blockIdx.x * WAVES + wave; s < b; s += gridDim.x * WAVES) {
         const int is = prefix[s];
         int rank = 0;
         if (is != kNoPrefix && is != kLeftOut)
@@ -216,7 +277,7 @@ __device__ __forceinline__ void shared_share(const SharedArgs& a, const SharedLi
 #pragma unroll
         for (int o = 32; o; o >>= 1) rank += __shfl_xor(rank, o, 64);
         if (lane == 0) {
-            SharedPlace to{-1, rank, 0, 0, 0, 0, before[b + s], (before[1 + b + s] - before[b + s]) / own_tiles};
+            SharedPlace to{-1, rank, 0, 0, 0, 0, own[s], (own[s + 1] - own[s]) / own_tiles};
             if (is != kLeftOut) to.row = a.rows.row_start ? a.rows.row_start[s + 1] - 1 : s;
             if (is != kNoPrefix && is != kLeftOut) {
                 to.members = members[is] - members[is - 1];
@@ -227,68 +288,87 @@ __device__ __forceinline__ void shared_share(const SharedArgs& a, const SharedLi
             a.place[s] = to;
         }
     }
-    if (blockIdx.x == 0 && tid == 0) *reinterpret_cast<int32_t*>(a.place + b) = total;
+    if (blockIdx.x == 0 && tid == 0) *reinterpret_cast<int2*>(a.place + b) = int2{total, own_total};
 
-    int x = shares.begin(share), e = 0;
-    const int x1 = shares.begin(share + 1);
-    for (int above = 2 * b; e + 1 < above;) {
-        const int mid = (e + above) >> 1;
-        if (before[mid] * a.h_kv <= x) e = mid; else above = mid;
-    }
-    e = __builtin_amdgcn_readfirstlane(e);
-    while (x < x1) {
-        const int e_before = __builtin_amdgcn_readfirstlane(before[e]), of_head = __builtin_amdgcn_readfirstlane(before[e + 1]) - e_before;
-        if (of_head == 0) {
-            ++e;
-            continue;
-        }
-        const bool is_prefix = e < b;
-        const int s = is_prefix ? e : e - b, at_member = __builtin_amdgcn_readfirstlane((int)members[is_prefix ? e : 0]),
-                  count = is_prefix ? __builtin_amdgcn_readfirstlane((int)members[e + 1]) - at_member : 1;
-        const int columns = count * a.group, width = is_prefix ? TILE : kOwn, tiles = (columns + width - 1) / width, steps = of_head / tiles;
-        const int in_e = x - e_before * a.h_kv, unit = in_e / steps, kv = unit / tiles, tile = unit - kv * tiles, first = in_e - unit * steps;
-        const int last = steps - first < x1 - x ? steps : first + (x1 - x), n = __builtin_amdgcn_readfirstlane(a.rows.cache_len[s]);
-        const int begin = first * kPagedStep, end = last == steps ? n : last * kPagedStep, here = columns - tile * width < width ? columns - tile * width : width;
-        const int64_t to = (int64_t)a.group * a.h_kv * (is_prefix ? at_member : b + s) + (int64_t)kv * columns + tile * width + (int64_t)share * kColumns;
-        const int32_t* const table = a.block_table + (int64_t)s * a.max_pages;
-        if (is_prefix) {
+    auto row_of = [&](int s) { return a.rows.row_start ? a.rows.row_start[s + 1] - 1 : s; };
+    auto prefixes = [&]() __attribute__((always_inline)) {
+        // (Shares that follow each other run on the same XCD, so that tiles of one prefix meet in its L2; where there is less than a step for each, all XCDs get some.)
+        const int share = total < a.shares ? blockIdx.x : (blockIdx.x & 7) * (a.shares >> 3) + (blockIdx.x >> 3), x1 = shares.begin(share + 1);
+        int x = shares.begin(share), e = x < x1 ? entry_of(before, b, a.h_kv, x) : 0;
+        while (x < x1) {
+            const int e_before = __builtin_amdgcn_readfirstlane(before[e]), of_head = __builtin_amdgcn_readfirstlane(before[e + 1]) - e_before;
+            if (of_head == 0) {
+                ++e;
+                continue;
+            }
+            const int at_member = __builtin_amdgcn_readfirstlane((int)members[e]), columns = (__builtin_amdgcn_readfirstlane((int)members[e + 1]) - at_member) * a.group,
+                      tiles = (columns + TILE - 1) / TILE, steps = of_head / tiles;
+            const int in_e = x - e_before * a.h_kv, unit = in_e / steps, kv = unit / tiles, tile = unit - kv * tiles, first = in_e - unit * steps;
+            const int last = steps - first < x1 - x ? steps : first + (x1 - x), n = __builtin_amdgcn_readfirstlane(a.rows.cache_len[e]);
+            const int begin = first * kPagedStep, end = last == steps ? n : last * kPagedStep, here = columns - tile * TILE < TILE ? columns - tile * TILE : TILE;
+            const int64_t to = (int64_t)a.group * a.h_kv * at_member + (int64_t)kv * columns + tile * TILE + (int64_t)share * TILE;
             // rows of the sequences whose heads are columns of this tile
             const int rank0 = tile * TILE / a.group, rank1 = (tile * TILE + here + a.group - 1) / a.group;
-            int own = 0;
-            for (int i = s0; i < s1; ++i) own += prefix[i] == e + 1;
-            int rank = sum_to(own, lists.scratch) - own;
+            int mine = 0, row = 0;
             for (int i = s0; i < s1; ++i)
                 if (prefix[i] == e + 1) {
-                    if (rank >= rank0 && rank < rank1) member_row[rank - rank0] = a.rows.row_start ? a.rows.row_start[i + 1] - 1 : i;
+                    if (mine++ == 0) row = row_of(i);
+                }
+            int rank = sum_to(mine, lists.scratch) - mine;
+            for (int i = s0, k = 0; i < s1; ++i)
+                if (prefix[i] == e + 1) {
+                    if (rank >= rank0 && rank < rank1) member_row[rank - rank0] = k == 0 ? row : row_of(i);
                     ++rank;
+                    ++k;
                 }
             __syncthreads();
-            prefix_part(table, kv, begin, end, here, [&](int i) __attribute__((always_inline)) {
+            prefix_part(a.block_table + (int64_t)e * a.max_pages, kv, begin, end, here, [&](int i) __attribute__((always_inline)) {
                 const int at = tile * TILE + i, rank = at / a.group;
                 return a.q + member_row[rank - rank0] * a.q_stride + ((int64_t)kv * a.group + at - rank * a.group) * (D * Elem<T>::kBytes);
             }, to);
-        } else {
-            const int row = a.rows.row_start ? a.rows.row_start[s + 1] - 1 : s;
-            const char* const heads = a.q + row * a.q_stride + ((int64_t)kv * a.group + tile * kOwn) * (D * Elem<T>::kBytes);
-            shared_part<T, C, D, OWN, WAVES>(a, table, kv, begin, end, here, lds, [&](int i) __attribute__((always_inline)) { return heads + (int64_t)i * (D * Elem<T>::kBytes); },
-                                             SharedEmit<D>{a.part_out, a.part_sum, to});
+            x += last - first;
+            if (x == (e_before + of_head) * a.h_kv) ++e;
         }
-        x += last - first;
-        if (x == (e_before + of_head) * a.h_kv) ++e;
-    }
+    };
+    auto sequences = [&]() __attribute__((always_inline)) {
+        // (the first shares of either kind are the ones with a step more: they are not the same workgroup's)
+        const int share = __builtin_amdgcn_readfirstlane((a.shares - 1 - (int)blockIdx.x) * WAVES + wave), x1 = own_shares.begin(share + 1);
+        int x = own_shares.begin(share), s = x < x1 ? entry_of(own, b, a.h_kv, x) : 0;
+        while (x < x1) {
+            const int s_before = __builtin_amdgcn_readfirstlane(own[s]), of_head = __builtin_amdgcn_readfirstlane(own[s + 1]) - s_before;
+            if (of_head == 0) {
+                ++s;
+                continue;
+            }
+            const int steps = of_head / own_tiles, in_s = x - s_before * a.h_kv, unit = in_s / steps, kv = unit / own_tiles, tile = unit - kv * own_tiles, first = in_s - unit * steps;
+            const int last = steps - first < x1 - x ? steps : first + (x1 - x);
+            if (last > 1) {                              // (a unit's first step has no tokens)
+                const int row = row_of(s), n = __builtin_amdgcn_readfirstlane(a.rows.cache_len[s]);
+                const int begin = first ? (first - 1) * kOwnStep : 0, end = last == steps ? n : (last - 1) * kOwnStep,
+                          here = a.group - tile * kOwnColumns < kOwnColumns ? a.group - tile * kOwnColumns : kOwnColumns;
+                own_part<T, C, D>(a, a.block_table + (int64_t)s * a.max_pages, kv, begin, end, here,
+                                  a.q + row * a.q_stride + ((int64_t)kv * a.group + tile * kOwnColumns) * (D * Elem<T>::kBytes),
+                                  a.own_columns + (int64_t)a.group * a.h_kv * s + (int64_t)kv * a.group + tile * kOwnColumns + (int64_t)share * kOwnColumns);
+            }
+            x += last - first;
+            if (x == (s_before + of_head) * a.h_kv) ++s;
+        }
+    };
+    sequences();
+    prefixes();
 }
 
 // 16 ROWS columns to a prefix's unit: all types, pages of any size.
-template <typename T, typename C, int D, int ROWS, int OWN>
+template <typename T, typename C, int D, int ROWS>
 __global__ void __launch_bounds__(256, Elem<C>::kBytes * D == 512 && ROWS == 2 ? 1 : 2) swa_paged_shared_kernel(SharedArgs a)
 {
     __shared__ SharedLds<D, 4> lds;
-    __shared__ int scratch[4], member_row[16 * ROWS + 1];
+    __shared__ int scratch[12], member_row[16 * ROWS + 1];
     extern __shared__ int lists[];
-    shared_share<T, C, D, 16 * ROWS, OWN, 4>(a, SharedLists(lists, a.b, scratch), member_row, lds,
-                                             [&](const int32_t* table, int kv, int begin, int end, int columns, auto from, int64_t to) __attribute__((always_inline)) {
-                                                 shared_part<T, C, D, ROWS, 4>(a, table, kv, begin, end, columns, lds, from, SharedEmit<D>{a.part_out, a.part_sum, to});
-                                             });
+    shared_share<T, C, D, 16 * ROWS, 4>(a, SharedLists(lists, a.b, scratch), member_row,
+                                        [&](const int32_t* table, int kv, int begin, int end, int columns, auto from, int64_t to) __attribute__((always_inline)) {
+                                            shared_part<T, C, D, ROWS, 4>(a, table, kv, begin, end, columns, lds, from, SharedEmit<D>{a.part_out, a.part_sum, to});
+                                        });
 }
 
 // ---- prefixes of many columns, 16 bit -------------------------------------------------------------------------------------------------------
@@ -297,7 +377,7 @@ __global__ void __launch_bounds__(256, Elem<C>::kBytes * D == 512 && ROWS == 2 ?
 // them, whose results meet in LDS at its end (two workgroups of four waves would leave twice as many partial results).  As in swa_flash.hip a lane owns one column throughout: S^T = K Q^T
 // leaves lane l the logits of 16 keys for column l % 32, O^T = V^T P^T takes its weights as they lie; key and value tiles go from L2 straight to LDS, three buffers of them,
 // two tiles ahead, rows permuted by chunks instead of padded.  A wave stages eight tokens that follow each other, which lie in one page where page_size is a
-// multiple of eight: their place is a scalar, and the table's entry a scalar load, one tile ahead of its use.
+// multiple of eight: their place is a scalar.
 //
 // Weights are rounded once to the cache's type here (two numbers for a weight, as in the decode, are half as many products again, and 16-bit outputs come 16 to 21 %
 // nearer to the exact ones, whose own rounding both have).  In fp16 they are raised by 2^11: the largest is below 2^15, one of 2^-25 of it a normal number still.
@@ -344,9 +424,9 @@ constexpr int wide_tile_bytes() { return 32 * D * 2; }
 template <int D>
 constexpr int wide_lds_bytes() { return 12 * wide_tile_bytes<D>() > kWideColumns * (D + 6) * 4 ? 12 * wide_tile_bytes<D>() : kWideColumns * (D + 6) * 4; }
 
-// Tokens begin .. end - 1 (begin a multiple of 32) for up to 128 columns.
+// Tokens begin .. end - 1 (begin a multiple of 32) for up to 128 columns.  False, and nothing is written: a page lies outside the pool (the first one stood in for it).
 template <typename T, int D, typename Q>
-__device__ __forceinline__ void wide_part(const SharedArgs& a, const int32_t* table_, int kv, int begin, int end, int columns, char* lds, Q from, int64_t to)
+__device__ __forceinline__ bool wide_part(const SharedArgs& a, const int32_t* table, int kv, int begin, int end, int columns, char* lds, Q from, int64_t to)
 {
     constexpr int kRow = D * 2, kTile = wide_tile_bytes<D>(), NV = kRow / 32, CT = D / 32, kChunks = kRow / 16, kRowsPerLoad = 64 / kChunks, LD = 8 / kRowsPerLoad, PF = 2;
     static_assert(2 * LD == NV / 2, "one load behind every second product of the first contraction");
@@ -356,9 +436,7 @@ __device__ __forceinline__ void wide_part(const SharedArgs& a, const int32_t* ta
     const int rounds = (end - begin + 63) >> 6;
     auto base_of = [&](int round) { return begin + round * 64 + half * 32; };
 
-    // The eight tokens that this wave stages of a round's tile (the last eight where there are none), and their page.
-    typedef const int32_t __attribute__((address_space(4))) * scalar_t;
-    const scalar_t table = (scalar_t)(uintptr_t)table_;
+    // The eight tokens that this wave stages of a round's tile (the last eight where there are none), and their page: lane i has that of round 64 k + i.
     const int last8 = (end - 1) & ~7;
     auto token_of = [&](int round) {
         const int t = base_of(round) + group * 8;
@@ -378,9 +456,17 @@ __device__ __forceinline__ void wide_part(const SharedArgs& a, const int32_t* ta
             offV[x] = (uint32_t)(r * kRow + (((ln % kChunks) ^ swzV(at)) << 4));
         }
     };
+    int pages = 0;
+    bool bad = false;
     int64_t at_row = 0;                                  // bytes before the eight rows in the pool
-    auto aim = [&](int round, int page) {
-        const int t = token_of(round);
+    auto aim = [&](int round) __attribute__((always_inline)) {
+        if ((round & 63) == 0) {
+            pages = table[page_of(token_of(round + lane))];
+            const bool in_pool = (uint32_t)pages < (uint32_t)a.n_pages;
+            bad |= !in_pool;
+            pages = in_pool ? pages : 0;
+        }
+        const int t = token_of(round), page = __builtin_amdgcn_readlane(pages, round & 63);
         at_row = ((int64_t)(page * a.h_kv + kv) * a.page_size + (t - page_of(t) * a.page_size)) * kRow;
         if (base_of(round) + 32 > end) offsets(end - 1 - t);
     };
@@ -390,8 +476,7 @@ __device__ __forceinline__ void wide_part(const SharedArgs& a, const int32_t* ta
     };
     offsets(8);
     __syncthreads();                                     // (what was in LDS before has been read)
-    int page = table[page_of(token_of(0))], next_page = table[page_of(token_of(1))];
-    aim(0, page);
+    aim(0);
 #pragma unroll
     for (int x = 0; x < 2 * LD; ++x) load(x, k0, v0);
     Vec16 q[NV];
@@ -407,9 +492,7 @@ __device__ __forceinline__ void wide_part(const SharedArgs& a, const int32_t* ta
     // (the queries are waited for here, where the compiler sees it, and not with the tiles requested since in every round)
     __builtin_amdgcn_s_waitcnt(0x0F70);                  // vmcnt(0)
     if (rounds > 1) {
-        page = next_page;
-        next_page = table[page_of(token_of(2))];
-        aim(1, page);
+        aim(1);
 #pragma unroll
         for (int x = 0; x < 2 * LD; ++x) load(x, k1, v1);
     }
@@ -424,10 +507,7 @@ __device__ __forceinline__ void wide_part(const SharedArgs& a, const int32_t* ta
 
     // tail: the round's tile may end inside; more: the tile two rounds on is requested
     auto compute = [&](bool tail, bool more, int round, const char* sk, const char* sv, char* nk, char* nv) __attribute__((always_inline)) {
-        if (more) {
-            aim(round + 2, next_page);
-            next_page = table[page_of(token_of(round + 3))];
-        }
+        if (more) aim(round + 2);
         if (!mine) {
             if (more)
 #pragma unroll
@@ -505,7 +585,7 @@ __device__ __forceinline__ void wide_part(const SharedArgs& a, const int32_t* ta
     float lo, hi;
     both_halves(l, lo, hi);
     l = lo + hi;
-    __syncthreads();
+    if (__syncthreads_or(bad)) return false;
 
     // The second half's results to the first's, and from there to memory, whole rows at a time.
     constexpr int kPitch = D + 4;
@@ -537,60 +617,56 @@ __device__ __forceinline__ void wide_part(const SharedArgs& a, const int32_t* ta
         const int r = i / (D / 4), c = i % (D / 4) * 4;
         *reinterpret_cast<f32x4_t*>(a.part_out + (to + r) * D + c) = *reinterpret_cast<const f32x4_t*>(result + r * kPitch + c);
     }
+    return true;
 }
 
-// (sequences' own tokens sixteen columns at a time: thirty-two would not fit the registers beside the rest)
 template <typename T, int D>
 __global__ void __launch_bounds__(512, 2) swa_paged_shared_wide_kernel(SharedArgs a)
 {
     extern __shared__ __align__(16) char lds[];          // tiles, then the lists
-    __shared__ int scratch[8], member_row[kWideColumns + 1];
+    __shared__ int scratch[24], member_row[kWideColumns + 1];
     SharedLds<D, 8>& sums = *reinterpret_cast<SharedLds<D, 8>*>(lds);
     static_assert(sizeof(SharedLds<D, 8>) <= wide_lds_bytes<D>(), "in the tiles' place");
-    shared_share<T, T, D, kWideColumns, 1, 8>(
-        a, SharedLists(reinterpret_cast<int*>(lds + wide_lds_bytes<D>()), a.b, scratch), member_row, sums,
+    shared_share<T, T, D, kWideColumns, 8>(
+        a, SharedLists(reinterpret_cast<int*>(lds + wide_lds_bytes<D>()), a.b, scratch), member_row,
         [&](const int32_t* table, int kv, int begin, int end, int columns, auto from, int64_t to) __attribute__((always_inline)) {
-            // (a page outside the pool is left out of the sums, which the other form of the work looks after)
-            bool bad = false;
-            for (int i = begin / a.page_size + (int)threadIdx.x; i <= (end - 1) / a.page_size; i += 512) bad |= (uint32_t)table[i] >= (uint32_t)a.n_pages;
-            if (!__syncthreads_or(bad)) {
-                wide_part<T, D>(a, table, kv, begin, end, columns, lds, from, to);
-            } else {
-                for (int c = 0; c < columns; c += 16)
-                    shared_part<T, T, D, 1, 8>(a, table, kv, begin, end, columns - c < 16 ? columns - c : 16, sums, [&](int i) __attribute__((always_inline)) { return from(c + i); },
-                                               SharedEmit<D>{a.part_out, a.part_sum, to + c});
-            }
+            if (wide_part<T, D>(a, table, kv, begin, end, columns, lds, from, to)) return;
+            // (what a page outside the pool would hold is left out of the sums, which the other form of the work looks after)
+            for (int c = 0; c < columns; c += 16)
+                shared_part<T, T, D, 1, 8>(a, table, kv, begin, end, columns - c < 16 ? columns - c : 16, sums, [&](int i) __attribute__((always_inline)) { return from(c + i); },
+                                           SharedEmit<D>{a.part_out, a.part_sum, to + c});
         });
 }
 
 // A query head's partial results, the prefix's and its own, to its output.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) swa_paged_join_shared_kernel(SharedArgs a, int tile, int own_tile)
+template <typename T, int D, int WAVES>
+__global__ void __launch_bounds__(256) swa_paged_join_shared_kernel(SharedArgs a, int tile, int waves)
 {
-    const int s = blockIdx.x / a.h_q, hq = blockIdx.x - s * a.h_q, kv = hq / a.group, head = hq - kv * a.group;
+    const int of = __builtin_amdgcn_readfirstlane(blockIdx.x * (4 / WAVES) + (WAVES == 1 ? threadIdx.x >> 6 : 0));
+    if (of >= a.b * a.h_q) return;
+    const int s = of / a.h_q, hq = of - s * a.h_q, kv = hq / a.group, head = hq - kv * a.group;
     const SharedPlace at = a.place[s];
     if (at.row < 0) return;
-    const PagedShares shares(*reinterpret_cast<const int32_t*>(a.place + a.b), a.shares);
-    const int width = tile > own_tile ? tile : own_tile;
-    int64_t first[2];
-    int count[2] = {0, 0};
-    auto unit = [&](int which, int x, int steps, int64_t columns) __attribute__((always_inline)) {
-        const int f = shares.of(x);
-        count[which] = shares.of(x + steps - 1) - f + 1;
-        first[which] = columns + (int64_t)f * width;
-    };
-    first[0] = first[1] = 0;
+    const int2 total = *reinterpret_cast<const int2*>(a.place + a.b);
+    int64_t first = 0, own_first = 0;
+    int count = 0, own_count = 0;
     if (at.prefix_steps > 0) {
         const int columns = at.members * a.group, i = at.rank * a.group + head, tiles = (columns + tile - 1) / tile;
-        unit(0, at.prefix_at * a.h_kv + (kv * tiles + i / tile) * at.prefix_steps, at.prefix_steps,
-             (int64_t)a.group * a.h_kv * at.first + (int64_t)kv * columns + i);
+        const int x = at.prefix_at * a.h_kv + (kv * tiles + i / tile) * at.prefix_steps;
+        const PagedShares shares(total.x, a.shares);
+        const int f = shares.of(x);
+        count = shares.of(x + at.prefix_steps - 1) - f + 1;
+        first = (int64_t)a.group * a.h_kv * at.first + (int64_t)kv * columns + i + (int64_t)f * tile;
     }
     if (at.steps > 0) {
-        const int tiles = (a.group + own_tile - 1) / own_tile;
-        unit(1, at.at * a.h_kv + (kv * tiles + head / own_tile) * at.steps, at.steps, (int64_t)a.group * a.h_kv * (a.b + s) + (int64_t)kv * a.group + head);
+        const int tiles = (a.group + kOwnColumns - 1) / kOwnColumns, x = at.at * a.h_kv + (kv * tiles + head / kOwnColumns) * at.steps;
+        const PagedShares shares(total.y, a.shares * waves);
+        const int f = shares.of(x + 1);                  // (of the first step with tokens)
+        own_count = shares.of(x + at.steps - 1) - f + 1;
+        own_first = a.own_columns + (int64_t)a.group * a.h_kv * s + (int64_t)kv * a.group + head + (int64_t)f * kOwnColumns;
     }
-    paged_join_pieces<T, D>(a.part_out, a.part_sum, [&](int i) __attribute__((always_inline)) { return i < count[0] ? first[0] + (int64_t)i * width : first[1] + (int64_t)(i - count[0]) * width; },
-                            count[0] + count[1], a.out, a.lse, (int64_t)at.row * a.h_q + hq);
+    paged_join_pieces<T, D, WAVES>(a.part_out, a.part_sum, [&](int i) __attribute__((always_inline)) { return i < count ? first + (int64_t)i * tile : own_first + (int64_t)(i - count) * kOwnColumns; },
+                            count + own_count, a.out, a.lse, (int64_t)at.row * a.h_q + hq);
 }
 
 // Columns that a prefix can have.
@@ -604,9 +680,11 @@ static int shared_rows(const swa_paged_params& p)
 }
 
 static int shared_shares(int rows) { return rows > 2 ? 256 : 512; }    // a workgroup to a CU, or two
+constexpr int kSharedWaves = 2048;                                     // of either
 
-// (whatever page_size a call states)
-static int64_t shared_columns(const swa_paged_params& p) { return 2 * (int64_t)p.b * p.h_q + (most_columns(p) > 32 ? 256 * kWideColumns : 512 * 32); }
+// Partial results of the prefixes, whatever page_size a call states, and of all.
+static int64_t prefix_columns(const swa_paged_params& p) { return (int64_t)p.b * p.h_q + (most_columns(p) > 32 ? 256 * kWideColumns : 512 * 32); }
+static int64_t shared_columns(const swa_paged_params& p) { return prefix_columns(p) + (int64_t)p.b * p.h_q + kSharedWaves * kOwnColumns; }
 
 size_t paged_shared_bytes(const swa_paged_params& p)
 {
@@ -614,10 +692,9 @@ size_t paged_shared_bytes(const swa_paged_params& p)
 }
 
 template <typename T, typename C, int D>
-static int launch_shared_form(const SharedArgs& a, int rows, int own, hipStream_t stream)
+static int launch_shared_form(const SharedArgs& a, int rows, hipStream_t stream)
 {
-    void (*kernel)(SharedArgs) = rows == 1 ? (own == 1 ? swa_paged_shared_kernel<T, C, D, 1, 1> : swa_paged_shared_kernel<T, C, D, 1, 2>)
-                                           : (own == 1 ? swa_paged_shared_kernel<T, C, D, 2, 1> : swa_paged_shared_kernel<T, C, D, 2, 2>);
+    void (*kernel)(SharedArgs) = rows == 1 ? swa_paged_shared_kernel<T, C, D, 1> : swa_paged_shared_kernel<T, C, D, 2>;
     size_t lds = shared_lists_bytes(a.b), of_its_own = 36 * 1024;
     int threads = 256;
     if constexpr (std::is_same_v<T, C> && !std::is_same_v<T, F32>) {
@@ -633,7 +710,9 @@ static int launch_shared_form(const SharedArgs& a, int rows, int own, hipStream_
         if (rc != SWA_OK) return rc;
     }
     launch_kernel(kernel, dim3((unsigned)a.shares), dim3(threads), lds, stream, a);
-    launch_kernel(swa_paged_join_shared_kernel<T, D>, dim3((unsigned)(a.b * a.h_q)), dim3(256), 0, stream, a, 16 * rows, 16 * own);
+    const unsigned heads = (unsigned)(a.b * a.h_q);
+    if (heads >= 1024) launch_kernel(swa_paged_join_shared_kernel<T, D, 1>, dim3((heads + 3) / 4), dim3(256), 0, stream, a, 16 * rows, threads / 64);
+    else launch_kernel(swa_paged_join_shared_kernel<T, D, 4>, dim3(heads), dim3(256), 0, stream, a, 16 * rows, threads / 64);
     return SWA_OK;
 }
 
@@ -664,12 +743,14 @@ int launch_paged_shared(const swa_paged_params& p, const swa_rows& q, int32_t n_
     a.group = p.h_q / p.h_kv;
     page_divisor(p.page_size, a.page_mul, a.page_shift);
     a.sixteens = p.page_size % 16 == 0;
-    const int rows = shared_rows(p), own = rows <= 2 && a.group > 16 ? 2 : 1;
+    const int rows = shared_rows(p);
     a.shares = shared_shares(rows);
+    a.own_columns = prefix_columns(p);
     // (steps are 32-bit numbers: of every sequence's own tokens, and of as many prefixes as may be)
-    const int64_t tiles = (int64_t)p.b * ((a.group + 16 * own - 1) / (16 * own)) + ((int64_t)p.b * a.group + 16 * rows - 1) / (16 * rows) + p.b;
-    if (tiles * p.h_kv > 0x7fffffffLL / ((a.rows.len_max + kPagedStep - 1) / kPagedStep) || (uint64_t)p.b * p.h_q * 256 > 0xffffffffULL) return SWA_ERR_CAPACITY;
-#define SWA_SHARED(T, C) (p.d == 64 ? launch_shared_form<T, C, 64>(a, rows, own, stream) : launch_shared_form<T, C, 128>(a, rows, own, stream))
+    const int64_t own_units = (int64_t)p.b * ((a.group + kOwnColumns - 1) / kOwnColumns) * p.h_kv,
+                  units = (((int64_t)p.b * a.group + 16 * rows - 1) / (16 * rows) + p.b) * p.h_kv, steps = ((int64_t)a.rows.len_max + kPagedStep - 1) / kPagedStep;
+    if (units > 0x7fffffffLL / steps || own_units > 0x7fffffffLL / (4 * steps + 1) || (uint64_t)p.b * p.h_q * 256 > 0xffffffffULL) return SWA_ERR_CAPACITY;
+#define SWA_SHARED(T, C) (p.d == 64 ? launch_shared_form<T, C, 64>(a, rows, stream) : launch_shared_form<T, C, 128>(a, rows, stream))
     const int rc = p.dtype == SWA_F32   ? SWA_SHARED(F32, F32)
                    : p.dtype == SWA_F16 ? (paged_int8(p) ? SWA_SHARED(F16, Q8) : SWA_SHARED(F16, F16))
                                         : (paged_int8(p) ? SWA_SHARED(BF16, Q8) : SWA_SHARED(BF16, BF16));

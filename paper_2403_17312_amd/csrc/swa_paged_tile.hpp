@@ -12,6 +12,7 @@
 #include <type_traits>
 
 #include "swa_paged.hpp"
+#include "swa_select.hpp"
 
 namespace swa {
 
@@ -135,20 +136,27 @@ struct PagedShares {
     }
 };
 
-// Sum of v up to and including this thread of a workgroup (scratch: one of LDS for each wave; all of them arrive).
-__device__ __forceinline__ int sum_to(int v, int* scratch)
+// Sums of N values up to and including this thread of a workgroup (scratch: N of LDS for each wave; all threads arrive).
+template <int N>
+__device__ __forceinline__ void sums_to(int (&v)[N], int* scratch)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int up = __shfl_up(v, o, 64);
-        if (lane >= o) v += up;
-    }
+    for (int i = 0; i < N; ++i) v[i] = wave_scan(v[i]);
     __syncthreads();
-    if (lane == 63) scratch[wave] = v;
+    if (lane == 63)
+#pragma unroll
+        for (int i = 0; i < N; ++i) scratch[wave * N + i] = v[i];
     __syncthreads();
-    for (int w = 0; w < wave; ++w) v += scratch[w];
-    return v;
+    for (int w = 0; w < wave; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += scratch[w * N + i];
+}
+__device__ __forceinline__ int sum_to(int v, int* scratch)
+{
+    int one[1] = {v};
+    sums_to(one, scratch);
+    return one[0];
 }
 
 // The pool, and the scale of logits to the base 2.
@@ -376,37 +384,58 @@ __device__ __forceinline__ void paged_join_waves(float (&part)[WAVES][16][D + 4]
     }
 }
 
-// Pieces of a query row, piece i at partial result piece_at(i), to its output, in their order.  A workgroup of 256 threads.
-template <typename T, int D, typename F>
+// Pieces of a query row, piece i at partial result piece_at(i), to its output, in an order that their number fixes.  By WAVES waves of a workgroup of 256 threads, of which
+// each has a row of its own where WAVES is 1.
+template <typename T, int D, int WAVES, typename F>
 __device__ __forceinline__ void paged_join_pieces(const float* part_out, const float* part_sum, F piece_at, int count, char* out, float* lse, int64_t to)
 {
-    constexpr int kLanes = D / 4, kTeams = 256 / kLanes;
-    const int tid = threadIdx.x, team = tid / kLanes, lane = tid % kLanes;
-    __shared__ float tops[kTeams], sums[kTeams];
-    __shared__ f32x4_t part[kTeams][kLanes];
+    constexpr int kLanes = D / 4, kTeams = 64 / kLanes, kAll = WAVES * kTeams;
+    const int tid = threadIdx.x & (64 * WAVES - 1), team = tid / kLanes, lane = tid % kLanes;
     float top = -INFINITY, total = 0.f;
     f32x4_t y = {0.f, 0.f, 0.f, 0.f};
-    auto join = [&](float most, float part_total, const f32x4_t& part_y) {
+    auto join = [&](float most, float part_total, const f32x4_t& part_y) __attribute__((always_inline)) {
         const float now = fmaxf(top, most), from = now == -INFINITY ? 0.f : now;
         const float old = __builtin_amdgcn_exp2f(top - from), w = __builtin_amdgcn_exp2f(most - from);
         y = y * old + part_y * w;
         total = total * old + part_total * w;
         top = now;
     };
-#pragma unroll 4
-    for (int i = team; i < count; i += kTeams) {
-        const int64_t at = piece_at(i);
-        const float2 m = *reinterpret_cast<const float2*>(part_sum + at * 2);
-        join(m.x, m.y, *reinterpret_cast<const f32x4_t*>(part_out + at * D + lane * 4));
+    constexpr int kAhead = 4;
+    for (int i = team; i < count; i += kAhead * kAll) {
+        float2 m[kAhead];
+        f32x4_t x[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t at = piece_at(i + k * kAll < count ? i + k * kAll : i);
+            m[k] = *reinterpret_cast<const float2*>(part_sum + at * 2);
+            x[k] = *reinterpret_cast<const f32x4_t*>(part_out + at * D + lane * 4);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k)
+            if (i + k * kAll < count) join(m[k].x, m[k].y, x[k]);
     }
-    part[team][lane] = y;
-    if (lane == 0) {
-        tops[team] = top;
-        sums[team] = total;
+    // the teams of a wave
+#pragma unroll
+    for (int o = kLanes; o < 64; o <<= 1) {
+        const f32x4_t other = {__shfl_xor(y[0], o, 64), __shfl_xor(y[1], o, 64), __shfl_xor(y[2], o, 64), __shfl_xor(y[3], o, 64)};
+        const float other_top = __shfl_xor(top, o, 64), other_total = __shfl_xor(total, o, 64);
+        join(other_top, other_total, other);
     }
-    __syncthreads();
-    if (team) return;
-    for (int i = 1; i < kTeams && i < count; ++i) join(tops[i], sums[i], part[i][lane]);
+    if constexpr (WAVES > 1) {
+        __shared__ float tops[WAVES], sums[WAVES];
+        __shared__ f32x4_t part[WAVES][kLanes];
+        const int wave = tid >> 6;
+        if (team % kTeams == 0) part[wave][lane] = y;
+        if ((tid & 63) == 0) {
+            tops[wave] = top;
+            sums[wave] = total;
+        }
+        __syncthreads();
+        if (wave) return;
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) join(tops[i], sums[i], part[i][lane]);
+    }
+    if (team % kTeams) return;
     const float out4[4] = {y[0], y[1], y[2], y[3]};
     paged_store<T, D>(out, lse, to, lane * 4, lane == 0, top, total, out4);
 }
