@@ -73,32 +73,56 @@ __global__ void __launch_bounds__(256) swa_paged_bounds_kernel(BoundsArgs a)
                 const int count = others ? (int)__builtin_ctzll(others) : 64;
                 const int32_t off = lane < count ? a.slot[mine] - page * a.page_size : 0;
                 fresh |= __ballot(lane < count && off == 0) != 0;
-                for (int i = 0; i < count; i += kTeams) {
-                    const int32_t there = __shfl(off, i + team < count ? i + team : i, 64);
-                    const Vec16 v = load16(a.k_pages + (row0 + there) * kRow + at * 16);
-                    float f[kVec];
-                    if constexpr (kCodes) {
-                        const float scale = a.k_scale[row0 + there];
+                constexpr int kAhead = 4;                // loads under way at once
+                for (int i = 0; i < count; i += kAhead * kTeams) {
+                    Vec16 v[kAhead];
+                    float scale[kAhead];
 #pragma unroll
-                        for (int x = 0; x < kVec; ++x) f[x] = (float)code_at(v, x) * scale;
-                    } else {
-                        unpack<C>(v, f);
+                    for (int k = 0; k < kAhead; ++k) {
+                        const int row = i + k * kTeams + team;           // (the last one again where there are no more)
+                        const int64_t at_row = row0 + __shfl(off, row < count ? row : count - 1, 64);
+                        v[k] = load16(a.k_pages + at_row * kRow + at * 16);
+                        if constexpr (kCodes) scale[k] = a.k_scale[at_row];
                     }
 #pragma unroll
-                    for (int x = 0; x < kVec; ++x) {
-                        lo[x] = least(lo[x], f[x]);
-                        hi[x] = most(hi[x], f[x]);
+                    for (int k = 0; k < kAhead; ++k) {
+                        float f[kVec];
+                        if constexpr (kCodes) {
+#pragma unroll
+                            for (int x = 0; x < kVec; ++x) f[x] = (float)code_at(v[k], x) * scale[k];
+                        } else {
+                            unpack<C>(v[k], f);
+                        }
+#pragma unroll
+                        for (int x = 0; x < kVec; ++x) {
+                            lo[x] = least(lo[x], f[x]);
+                            hi[x] = most(hi[x], f[x]);
+                        }
                     }
                 }
                 if (count < 64) break;
             }
+            // the teams to one: lanes 8, 16 and 32 apart, as far as these are teams
 #pragma unroll
-            for (int o = kLanes; o < 64; o <<= 1)
-#pragma unroll
-                for (int x = 0; x < kVec; ++x) {
-                    lo[x] = least(lo[x], __shfl_xor(lo[x], o, 64));
-                    hi[x] = most(hi[x], __shfl_xor(hi[x], o, 64));
+            for (int x = 0; x < kVec; ++x) {
+                if constexpr (kLanes <= 4) {
+                    lo[x] = least(lo[x], __shfl_xor(lo[x], 4, 64));
+                    hi[x] = most(hi[x], __shfl_xor(hi[x], 4, 64));
                 }
+                if constexpr (kLanes <= 8) {
+                    lo[x] = least(lo[x], dpp_move<0x128>(lo[x]));        // row_ror 8
+                    hi[x] = most(hi[x], dpp_move<0x128>(hi[x]));
+                }
+                if constexpr (kLanes <= 16) {
+                    lo[x] = least(lo[x], __shfl_xor(lo[x], 16, 64));
+                    hi[x] = most(hi[x], __shfl_xor(hi[x], 16, 64));
+                }
+                float a0, a1;
+                both_halves(lo[x], a0, a1);
+                lo[x] = least(a0, a1);
+                both_halves(hi[x], a0, a1);
+                hi[x] = most(a0, a1);
+            }
             if (team) continue;
             constexpr int kT = Elem<T>::kBytes, kPer = Elem<T>::kPerVec;
             char* const to = a.bounds + ((int64_t)page * a.h_kv + head) * (2 * D * kT) + at * kVec * kT;
