@@ -144,7 +144,7 @@ typedef struct {
 
 /*
  * One-time set-up on the current device, optional but needed before stream capture: raises the
- * LDS limit of every decode kernel to the device's maximum and looks up the scratch array of
+ * LDS limit of every decode kernel (swa_paged_decode_shared's too) to the device's maximum and looks up the scratch array of
  * swa_decode_step_static.  Host-side only; enqueues nothing.  Call it again after hipSetDevice
  * to another GPU.
  */

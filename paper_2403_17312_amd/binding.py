@@ -552,13 +552,16 @@ def swa_paged_decode_shared(params: SwaPagedParams, q, n_rows: int, row_start, s
 class PagedCache:
     """Device tensors of a paged cache: one pool per layer, one plan for all of them (allocation plumbing, and checks of what is
     handed in).  A step is plan(), then append() and decode() for every layer.  plan() swaps the two copies of the lengths and of the ring's
-    state, so a captured step replays with the copies that it was captured with: capture two steps and replay them in turn."""
+    state, so a captured step replays with the copies that it was captured with: capture two steps and replay them in turn.
+    select: the pages that decode_sparse() reads of a sequence at most; append() then keeps the bounds of the pages' keys, too."""
 
-    def __init__(self, params: SwaPagedParams, layers: int = 1, device="cuda"):
+    def __init__(self, params: SwaPagedParams, layers: int = 1, device="cuda", select: int = 0):
         p = self.params = params
         nbytes = swa_paged_workspace_bytes(p)
         if not nbytes:
             raise ValueError("no paged cache has these parameters")
+        if select and (not 1 <= select <= p.max_pages or p.window):
+            raise ValueError("select is 0, or a number of pages up to max_pages in a cache without a window")
         self.dtype = {v: k for k, v in DTYPE_CODE.items()}[p.dtype]
         int8 = bool(p.flags & SWA_KV_INT8)
         shape = (p.n_pages, p.h_kv, p.page_size, p.d)
@@ -576,6 +579,12 @@ class PagedCache:
         self._slot = None                              # of the last plan
         self.workspace = torch.zeros((nbytes,), dtype=torch.uint8, device=device)
         swa_paged_workspace_init(p, self.workspace)
+        self.select = select
+        if select:
+            self.bounds = pools((p.n_pages, p.h_kv, 2, p.d), self.dtype)
+            self.score = torch.zeros((p.b, p.h_kv, p.max_pages), dtype=torch.float32, device=device)
+            self.sel = torch.full((p.b, p.h_kv, select), -1, dtype=torch.int32, device=device)
+            self.sel_cnt = torch.zeros((p.b, p.h_kv), dtype=torch.int32, device=device)
 
     def _expect(self, name, t, shape, dtype) -> None:
         if tuple(t.shape) != tuple(shape) or t.dtype != dtype:
@@ -609,20 +618,49 @@ class PagedCache:
                 self._expect(name, w, (p.d,), self.dtype)
         swa_paged_append(p, q, k, v, n, pos, slot, inv_freq, q_weight, k_weight, q_out, self.k_pages[layer], self.v_pages[layer],
                          self.k_scale[layer], self.v_scale[layer], self.workspace, stream)
+        if self.select:
+            swa_paged_bounds(p, n, slot, self.k_pages[layer], self.k_scale[layer], self.bounds[layer], self.workspace, stream)
 
-    def decode(self, layer: int, q, out, lse=None, by_rows: bool = False, stream=None) -> None:
-        """by_rows: q and out hold the plan's packed rows, and each sequence's last one is meant; nothing is written for a sequence that the plan
-        has refused (its slots, which still hold what plan() wrote, say so).  Otherwise row s is sequence s, whether it was refused or not."""
+    def _queries(self, q, out, lse, by_rows: bool):
+        """Rows of a call, and the lists that say whose they are."""
         p, n = self.params, q.shape[0]
         self._expect("q", q, (n, p.h_q, p.d), self.dtype)
         self._expect("out", out, (n, p.h_q, p.d), self.dtype)
         if lse is not None:
             self._expect("lse", lse, (n, p.h_q), torch.float32)
-        cache = (self.k_pages[layer], self.v_pages[layer], self.k_scale[layer], self.v_scale[layer], self.block_table, self.cache_len)
-        if by_rows and self._slot is not None:
-            swa_paged_decode_planned(p, q, min(n, self._slot.numel()), self.row_start, self._slot, *cache, out, lse, self.workspace, stream)
+        if not by_rows:
+            return n, None, None
+        return (n if self._slot is None else min(n, self._slot.numel())), self.row_start, self._slot
+
+    def decode(self, layer: int, q, out, lse=None, by_rows: bool = False, stream=None) -> None:
+        """by_rows: q and out hold the plan's packed rows, and each sequence's last one is meant; nothing is written for a sequence that the plan
+        has refused (its slots, which still hold what plan() wrote, say so).  Otherwise row s is sequence s, whether it was refused or not."""
+        n, rows, slot = self._queries(q, out, lse, by_rows)
+        if slot is not None:
+            swa_paged_decode_planned(self.params, q, n, rows, slot, *self._cache(layer), out, lse, self.workspace, stream)
         else:
-            swa_paged_decode(p, q, n, self.row_start if by_rows else None, *cache, out, lse, self.workspace, stream)
+            swa_paged_decode(self.params, q, n, rows, *self._cache(layer), out, lse, self.workspace, stream)
+
+    def _cache(self, layer: int):
+        return self.k_pages[layer], self.v_pages[layer], self.k_scale[layer], self.v_scale[layer], self.block_table, self.cache_len
+
+    def decode_sparse(self, layer: int, q, out, first: int = 1, last: int = 2, lse=None, by_rows: bool = False, stream=None) -> None:
+        """decode() over `select` pages of each sequence and key head: the `first` first ones, the `last` last ones, and those whose bounds promise the largest
+        logits (score, sel and sel_cnt hold what was found, until the next call)."""
+        if not self.select:
+            raise ValueError("this cache keeps no bounds: PagedCache(..., select=...)")
+        n, rows, slot = self._queries(q, out, lse, by_rows)
+        p, ws = self.params, self.workspace
+        swa_paged_score(p, q, n, rows, slot, self.bounds[layer], self.block_table, self.cache_len, self.score, ws, stream)
+        swa_paged_select(p, self.score, self.cache_len, self.select, first, last, self.sel, self.sel_cnt, ws, stream)
+        swa_paged_decode_selected(p, q, n, rows, slot, *self._cache(layer), self.sel, self.sel_cnt, self.select, out, lse, ws, stream)
+
+    def decode_shared(self, layer: int, q, out, prefix_of, lse=None, by_rows: bool = False, stream=None) -> None:
+        """decode() where the tokens of sequence prefix_of[s] (-1: none) come before those of sequence s.  A prefix is planned and appended like any sequence; the
+        positions of those behind it are the plan's plus its length."""
+        n, rows, slot = self._queries(q, out, lse, by_rows)
+        self._expect("prefix_of", prefix_of, (self.params.b,), torch.int32)
+        swa_paged_decode_shared(self.params, q, n, rows, slot, *self._cache(layer), prefix_of, out, lse, self.workspace, stream)
 
     def check_status(self, stream=None) -> int:
         return swa_paged_check_status(self.params, self.workspace, stream)

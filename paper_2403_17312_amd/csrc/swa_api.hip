@@ -10,6 +10,7 @@
 #include <unordered_map>
 
 #include "swa_kernels.hpp"
+#include "swa_paged.hpp"
 
 namespace swa {
 
@@ -302,7 +303,8 @@ int swa_prepare(void)
     int rc = swa::static_scratch(&ptr);
     if (rc != SWA_OK) return rc;
     rc = swa::prepare_decode();
-    return rc;
+    if (rc != SWA_OK) return rc;
+    return swa::prepare_paged_shared();
 }
 
 int swa_check_status(const swa_params* params, void* workspace, void* stream, int32_t* status_out)

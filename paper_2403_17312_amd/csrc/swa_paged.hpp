@@ -84,6 +84,9 @@ int launch_paged_selected(const swa_paged_params& p, const swa_rows& q, int32_t 
 // Bytes of the partial results of swa_paged_decode_shared, which lie where those of swa_paged_decode do.
 size_t paged_shared_bytes(const swa_paged_params& p);
 
+// Raises the LDS limit of its kernels on the current device.
+int prepare_paged_shared();
+
 int launch_paged_shared(const swa_paged_params& p, const swa_rows& q, int32_t n_rows, const int32_t* row_start, const int32_t* slot,
                         const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale, const int32_t* block_table,
                         const int32_t* cache_len, const int32_t* prefix_of, void* out, float* lse, void* workspace, hipStream_t stream);

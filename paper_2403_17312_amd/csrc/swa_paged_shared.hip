@@ -716,6 +716,28 @@ static int launch_shared_form(const SharedArgs& a, int rows, hipStream_t stream)
     return SWA_OK;
 }
 
+template <typename T, typename C, int D>
+static int prepare_shared_form()
+{
+    for (void (*kernel)(SharedArgs) : {swa_paged_shared_kernel<T, C, D, 1>, swa_paged_shared_kernel<T, C, D, 2>}) {
+        const int rc = raise_dynamic_lds(reinterpret_cast<const void*>(kernel));
+        if (rc != SWA_OK) return rc;
+    }
+    if constexpr (std::is_same_v<T, C> && !std::is_same_v<T, F32>) return raise_dynamic_lds(reinterpret_cast<const void*>(swa_paged_shared_wide_kernel<T, D>));
+    return SWA_OK;
+}
+
+int prepare_paged_shared()
+{
+    for (int (*form)() : {prepare_shared_form<F32, F32, 64>, prepare_shared_form<F32, F32, 128>, prepare_shared_form<F16, F16, 64>, prepare_shared_form<F16, F16, 128>,
+                          prepare_shared_form<F16, Q8, 64>, prepare_shared_form<F16, Q8, 128>, prepare_shared_form<BF16, BF16, 64>, prepare_shared_form<BF16, BF16, 128>,
+                          prepare_shared_form<BF16, Q8, 64>, prepare_shared_form<BF16, Q8, 128>}) {
+        const int rc = form();
+        if (rc != SWA_OK) return rc;
+    }
+    return SWA_OK;
+}
+
 int launch_paged_shared(const swa_paged_params& p, const swa_rows& q, int32_t n_rows, const int32_t* row_start, const int32_t* slot,
                         const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale, const int32_t* block_table,
                         const int32_t* cache_len, const int32_t* prefix_of, void* out, float* lse, void* workspace, hipStream_t stream)
