@@ -70,7 +70,7 @@ struct SharedLds {
 };
 
 // Tokens begin .. end - 1 of the pages in `table`, for query columns whose rows begin at from(column).
-template <typename T, typename C, int D, int ROWS, int WAVES, typename Q, typename F>
+template <typename T, typename C, int D, int ROWS, int WAVES, bool STREAM, typename Q, typename F>
 __device__ __forceinline__ void shared_part(const SharedArgs& a, const int32_t* table, int kv, int begin, int end, int columns, SharedLds<D, WAVES>& lds, Q from, F emit)
 {
     typedef PagedTile<T, C, D, ROWS> S;
@@ -116,7 +116,7 @@ __device__ __forceinline__ void shared_part(const SharedArgs& a, const int32_t* 
             if (next < end) page = table[page_of(next)];
             const int rows = row_of(base, this_page);
             if (!__any(rows < 0)) {
-                paged_take<T, C, D, ROWS, true>(a.pool, rows, q, top, sum, acc);
+                paged_take<T, C, D, ROWS, true, STREAM>(a.pool, rows, q, top, sum, acc);
             } else {
                 if (left == end) {
                     left = base;
@@ -129,7 +129,7 @@ __device__ __forceinline__ void shared_part(const SharedArgs& a, const int32_t* 
         r = row_of(next, page);
     }
     while (left < left_end) {
-        paged_take<T, C, D, ROWS, false>(a.pool, r, q, top, sum, acc);
+        paged_take<T, C, D, ROWS, false, STREAM>(a.pool, r, q, top, sum, acc);
         do {
             left += kStride;
             if (left >= left_end) break;
@@ -358,8 +358,9 @@ __device__ __forceinline__ void shared_share(const SharedArgs& a, const SharedLi
     prefixes();
 }
 
-// 16 ROWS columns to a prefix's unit: all types, pages of any size.
-template <typename T, typename C, int D, int ROWS>
+// 16 ROWS columns to a prefix's unit: all types, pages of any size.  STREAM: prefixes have one unit a key head; else their tiles' loads stay in the caches for the next one (us, 128
+// sequences of 16 to 300 tokens behind 8192, 32 query and 8 key heads of 128 channels: 8-bit codes 76.1 / 65.9, bf16 in pages of 20 104 / 79; 64 in fp32 121 / 111).
+template <typename T, typename C, int D, int ROWS, bool STREAM>
 __global__ void __launch_bounds__(256, Elem<C>::kBytes * D == 512 && ROWS == 2 ? 1 : 2) swa_paged_shared_kernel(SharedArgs a)
 {
     __shared__ SharedLds<D, 4> lds;
@@ -367,7 +368,7 @@ __global__ void __launch_bounds__(256, Elem<C>::kBytes * D == 512 && ROWS == 2 ?
     extern __shared__ int lists[];
     shared_share<T, C, D, 16 * ROWS, 4>(a, SharedLists(lists, a.b, scratch), member_row,
                                         [&](const int32_t* table, int kv, int begin, int end, int columns, auto from, int64_t to) __attribute__((always_inline)) {
-                                            shared_part<T, C, D, ROWS, 4>(a, table, kv, begin, end, columns, lds, from, SharedEmit<D>{a.part_out, a.part_sum, to});
+                                            shared_part<T, C, D, ROWS, 4, STREAM>(a, table, kv, begin, end, columns, lds, from, SharedEmit<D>{a.part_out, a.part_sum, to});
                                         });
 }
 
@@ -633,7 +634,7 @@ __global__ void __launch_bounds__(512, 2) swa_paged_shared_wide_kernel(SharedArg
             if (wide_part<T, D>(a, table, kv, begin, end, columns, lds, from, to)) return;
             // (what a page outside the pool would hold is left out of the sums, which the other form of the work looks after)
             for (int c = 0; c < columns; c += 16)
-                shared_part<T, T, D, 1, 8>(a, table, kv, begin, end, columns - c < 16 ? columns - c : 16, sums, [&](int i) __attribute__((always_inline)) { return from(c + i); },
+                shared_part<T, T, D, 1, 8, false>(a, table, kv, begin, end, columns - c < 16 ? columns - c : 16, sums, [&](int i) __attribute__((always_inline)) { return from(c + i); },
                                            SharedEmit<D>{a.part_out, a.part_sum, to + c});
         });
 }
@@ -692,9 +693,9 @@ size_t paged_shared_bytes(const swa_paged_params& p)
 }
 
 template <typename T, typename C, int D>
-static int launch_shared_form(const SharedArgs& a, int rows, hipStream_t stream)
+static int launch_shared_form(const SharedArgs& a, int rows, bool again, hipStream_t stream)
 {
-    void (*kernel)(SharedArgs) = rows == 1 ? swa_paged_shared_kernel<T, C, D, 1> : swa_paged_shared_kernel<T, C, D, 2>;
+    void (*kernel)(SharedArgs) = rows == 1 ? swa_paged_shared_kernel<T, C, D, 1, true> : again ? swa_paged_shared_kernel<T, C, D, 2, false> : swa_paged_shared_kernel<T, C, D, 2, true>;
     size_t lds = shared_lists_bytes(a.b), of_its_own = 36 * 1024;
     int threads = 256;
     if constexpr (std::is_same_v<T, C> && !std::is_same_v<T, F32>) {
@@ -719,7 +720,7 @@ static int launch_shared_form(const SharedArgs& a, int rows, hipStream_t stream)
 template <typename T, typename C, int D>
 static int prepare_shared_form()
 {
-    for (void (*kernel)(SharedArgs) : {swa_paged_shared_kernel<T, C, D, 1>, swa_paged_shared_kernel<T, C, D, 2>}) {
+    for (void (*kernel)(SharedArgs) : {swa_paged_shared_kernel<T, C, D, 1, true>, swa_paged_shared_kernel<T, C, D, 2, true>, swa_paged_shared_kernel<T, C, D, 2, false>}) {
         const int rc = raise_dynamic_lds(reinterpret_cast<const void*>(kernel));
         if (rc != SWA_OK) return rc;
     }
@@ -766,13 +767,14 @@ int launch_paged_shared(const swa_paged_params& p, const swa_rows& q, int32_t n_
     page_divisor(p.page_size, a.page_mul, a.page_shift);
     a.sixteens = p.page_size % 16 == 0;
     const int rows = shared_rows(p);
+    const bool again = most_columns(p) > 32;             // a prefix may have several units a key head
     a.shares = shared_shares(rows);
     a.own_columns = prefix_columns(p);
     // (steps are 32-bit numbers: of every sequence's own tokens, and of as many prefixes as may be)
     const int64_t own_units = (int64_t)p.b * ((a.group + kOwnColumns - 1) / kOwnColumns) * p.h_kv,
                   units = (((int64_t)p.b * a.group + 16 * rows - 1) / (16 * rows) + p.b) * p.h_kv, steps = ((int64_t)a.rows.len_max + kPagedStep - 1) / kPagedStep;
     if (units > 0x7fffffffLL / steps || own_units > 0x7fffffffLL / (4 * steps + 1) || (uint64_t)p.b * p.h_q * 256 > 0xffffffffULL) return SWA_ERR_CAPACITY;
-#define SWA_SHARED(T, C) (p.d == 64 ? launch_shared_form<T, C, 64>(a, rows, stream) : launch_shared_form<T, C, 128>(a, rows, stream))
+#define SWA_SHARED(T, C) (p.d == 64 ? launch_shared_form<T, C, 64>(a, rows, again, stream) : launch_shared_form<T, C, 128>(a, rows, again, stream))
     const int rc = p.dtype == SWA_F32   ? SWA_SHARED(F32, F32)
                    : p.dtype == SWA_F16 ? (paged_int8(p) ? SWA_SHARED(F16, Q8) : SWA_SHARED(F16, F16))
                                         : (paged_int8(p) ? SWA_SHARED(BF16, Q8) : SWA_SHARED(BF16, BF16));

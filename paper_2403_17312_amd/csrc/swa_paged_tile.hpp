@@ -168,8 +168,8 @@ struct PagedPool {
 
 // One tile, whose tokens lie in rows r (of lane t % kKeys) of the pool.  In `whole` tiles all of them do, and sixteen at a time behind each
 // other, so that addresses are a scalar and a lane's constant; in others each lane fetches its rows' numbers, and rows of -1 are left out.
-// top and sum: of column lane % 16, the sum of this lane's keys alone.
-template <typename T, typename C, int D, int ROWS, bool kWhole>
+// top and sum: of column lane % 16, the sum of this lane's keys alone.  STREAM: nobody reads the tile again.
+template <typename T, typename C, int D, int ROWS, bool kWhole, bool STREAM = true>
 __device__ __forceinline__ void paged_take(const PagedPool& a, const int r, const Vec16 (&q)[ROWS][PagedTile<T, C, D, ROWS>::kSteps], float (&top)[ROWS],
                                            float (&sum)[ROWS], f32x4_t (&acc)[ROWS][PagedTile<T, C, D, ROWS>::kChannels])
 {
@@ -194,7 +194,7 @@ __device__ __forceinline__ void paged_take(const PagedPool& a, const int r, cons
             k_from = a.k_pages + (int64_t)(rk < 0 ? 0 : rk) * kRow + j * 16;
         }
 #pragma unroll
-        for (int c = 0; c < kLoads; ++c) k[u][c] = load16_stream(k_from + c * 64);
+        for (int c = 0; c < kLoads; ++c) k[u][c] = STREAM ? load16_stream(k_from + c * 64) : load16(k_from + c * 64);
     }
 #pragma unroll
     for (int u = 0; u < kTiles; ++u) {
@@ -209,7 +209,7 @@ __device__ __forceinline__ void paged_take(const PagedPool& a, const int r, cons
                 v_from = a.v_pages + (int64_t)(rv[u][i] < 0 ? 0 : rv[u][i]) * kRow + col * kVBytes;
             }
 #pragma unroll
-            for (int x = 0; x < kVLoad; ++x) v[u][i][x] = load_values<Values>(v_from + x * 256);
+            for (int x = 0; x < kVLoad; ++x) v[u][i][x] = STREAM ? load_values<Values>(v_from + x * 256) : *reinterpret_cast<const Values*>(v_from + x * 256);
         }
         if constexpr (kCodes) {
             if constexpr (kWhole) {
