@@ -6,8 +6,9 @@
 #include <stdio.h>
 #include <stdlib.h>
 
+#include <map>
 #include <mutex>
-#include <unordered_map>
+#include <utility>
 
 #include "swa_kernels.hpp"
 #include "swa_paged.hpp"
@@ -18,15 +19,21 @@ int ensure_dynamic_lds(const void* kernel, size_t bytes)
 {
     if (bytes <= 48 * 1024) return SWA_OK;
     static std::mutex mu;
-    static std::unordered_map<const void*, size_t> granted;
+    static std::map<std::pair<const void*, int>, size_t> granted;        // of a kernel on a device
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) {
+        (void)hipGetLastError();
+        return SWA_ERR_HIP;
+    }
+    const std::pair<const void*, int> key(kernel, dev);
     std::lock_guard<std::mutex> lock(mu);
-    auto it = granted.find(kernel);
+    auto it = granted.find(key);
     if (it != granted.end() && it->second >= bytes) return SWA_OK;
     if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) {
         (void)hipGetLastError();
         return SWA_ERR_CAPACITY;
     }
-    granted[kernel] = bytes;
+    granted[key] = bytes;
     return SWA_OK;
 }
 
