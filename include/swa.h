@@ -584,7 +584,7 @@ int swa_paged_decode_planned(const swa_paged_params *params, swa_rows q, int32_t
  *
  * swa_paged_bounds: for every row r < n_rows with slot[r] >= 0, after swa_paged_append has written it:
  *   bounds[page][head][0][c] = min, [1][c] = max of K[c] over the page's tokens, of those that it had and the call's; a page whose first token
- *   (offset 0) is among the call's begins anew.  Values are the cache's (with SWA_KV_INT8 code times scale in fp32, rounded to dtype); what is no number stays
+ *   (offset 0) is among the call's begins anew (a wave takes all of a page's new tokens: pages are meant to be of some hundred at most).  Values are the cache's (with SWA_KV_INT8 code times scale in fp32, rounded to dtype); what is no number stays
  *   in them.  The rows of one page follow each other in `slot` (as swa_paged_plan makes them).  The same call again gives the same bounds.
  *   A slot outside the pool is left out and sets the SWA_ERR_BAD_REQUEST bit.
  *   slot [n_rows], k_pages, k_scale (in); bounds [n_pages, h_kv, 2, d] dtype (in/out), 16-byte aligned.
@@ -619,7 +619,7 @@ int swa_paged_select(const swa_paged_params *params, const float *score, const i
  * swa_paged_decode over the tokens of listed pages alone: those of pages sel[s][h][0 .. sel_cnt[s][h]) for the query heads of key head h.  lse is theirs, too.
  * Entries below zero, and those of pages without tokens, count for nothing; entries of max_pages and more, pages outside the pool and a sel_cnt outside
  * 0..n_sel (which counts as the nearer end) set the SWA_ERR_BAD_REQUEST bit.  A page listed twice counts twice.  Without tokens, out = 0 and lse = -inf.
- * Everything else is as there, the roundings and skipped sequences too; the launch goes by n_sel * page_size tokens.
+ * Everything else is as there, the roundings and skipped sequences too; the launch goes by n_sel * page_size tokens, and b * h_q is below 2^24 (SWA_ERR_CAPACITY).
  */
 int swa_paged_decode_selected(const swa_paged_params *params, swa_rows q, int32_t n_rows, const int32_t *row_start, const int32_t *slot,
                               const void *k_pages, const void *v_pages, const float *k_scale, const float *v_scale,
@@ -631,11 +631,12 @@ int swa_paged_decode_selected(const swa_paged_params *params, swa_rows q, int32_
  * alone).  A prefix is a sequence of the same cache, planned and appended like any other, of which further rows of the table need no copy; its keys and
  * values are read once for all the sequences behind it, not once for each.  Positions that swa_paged_plan gives count a sequence's own tokens, so the caller adds
  * the prefix's length to them before swa_paged_append.  A prefix that is kept and not decoded has no rows in row_start (new_cnt 0).
- *   out[r] = softmax over the tokens of both, lse likewise; r, row_start, slot and skipped sequences as in swa_paged_decode_selected.
+ *   out[r] = softmax over the tokens of both times their values, lse likewise; r, row_start, slot and skipped sequences as in swa_paged_decode_selected.
  * One prefix counts: prefix_of[prefix_of[s]] is not looked at.  Sequences whose prefix is none (outside 0..b-1, s itself, or an unused row with a negative
  * cache_len) are skipped and set the SWA_ERR_BAD_REQUEST bit; those of a prefix that is longer than its table or a stated len_bound are skipped and set the
- * SWA_ERR_CAPACITY bit.  params->window is 0.  Roundings as in swa_paged_decode; a sequence's results may differ in their last bits with the call's others, whose
- * lengths and prefixes say where tokens are cut into pieces.
+ * SWA_ERR_CAPACITY bit.  params->window is 0.  Roundings as in swa_paged_decode, but for a prefix's weights where (b - 1) * h_q / h_kv is above 32 with 16-bit pages of
+ * a multiple of eight tokens: these are rounded once to dtype (in fp16 in steps of 2^-35 of the largest, or finer).  A sequence's results may differ in their last bits with
+ * the call's others, whose lengths and prefixes say where tokens are cut into pieces.
  * SWA_ERR_CAPACITY also for more than a launch holds: 2^24 of b * h_q, and about 2^31 of h_kv * (2 b + b * h_q / h_kv / 32) * len / 128 with len the
  * longest sequence (of its table, len_bound).
  *   prefix_of [b] int32 (in).

@@ -2,7 +2,7 @@
 //   q . k = sum_c q_c k_c <= sum_c max(q_c, 0) hi_c + min(q_c, 0) lo_c,
 // a product of a row of 2 D bounds with the query's negative and positive parts, so it goes to the matrix cores like the attention's logits: sixteen
 // rows of bounds by sixteen query heads.  Bound: HBM, one read of the bounds, where calls are large: 32 sequences of 1000 to 65536 tokens in pages of 16, 8 key heads of 128 bf16
-// channels 52 us, 5.3 TB/s.  (With a load's lanes where the products want them, sixteen pieces of 64 bytes each, 96 us; more waves, or whole pages to a load, gain
+// channels 51 us, 5.4 TB/s.  (With a load's lanes where the products want them, sixteen pieces of 64 bytes each, 96 us; more waves, or whole pages to a load, gain
 // nothing.)
 #include "swa_paged_tile.hpp"
 

@@ -1,5 +1,6 @@
 // The pages that a sequence's attention reads: its first ones, its last ones, and of those between the ones of highest score, ties to the lowest page; in
-// ascending order.  Bound: latency, a chain of counts and barriers of one workgroup for each sequence and key head.
+// ascending order.  Bound: latency, a chain of counts and barriers of one workgroup for each sequence and key head: 500 pages 4.5 us, of which a launch is 3.5; 8192 in
+// 1024 threads 10.3 (in 512 10.6, in 256 15.1).
 //
 // A thread holds pages that follow each other, so that its place in the list is one running sum over the threads.  The threshold comes from a histogram select
 // over the keys' own range (swa_select.hpp).

@@ -1,5 +1,6 @@
 // Attention of one new token per sequence over pages that a list names, for each key head its own (as swa_paged_select writes them).  Bound by HBM: the listed
-// tokens' keys and values are read once.
+// tokens' keys and values are read once: 64 sequences of 8 key heads, 2048 tokens each of 128 bf16 channels, 89 us, 6.0 TB/s (of 7.2 that a read stream reaches); with six
+// waves to a workgroup 92, in chunks of half the tokens 92.5.  8-bit codes are bound by their conversion besides, as in the decode.
 //
 // The lists' tokens, page behind page, are a sequence like any other, and the workgroup's work is the decode's (swa_paged_tile.hpp): up to 16 (or 32) query heads of a
 // key head over a chunk of it.  Lists are about equally long whatever the sequences are, so chunks are, too, and no workgroup needs to know the other ones'
