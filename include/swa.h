@@ -584,8 +584,9 @@ int swa_paged_decode_planned(const swa_paged_params *params, swa_rows q, int32_t
  *
  * swa_paged_bounds: for every row r < n_rows with slot[r] >= 0, after swa_paged_append has written it:
  *   bounds[page][head][0][c] = min, [1][c] = max of K[c] over the page's tokens, of those that it had and the call's; a page whose first token
- *   (offset 0) is among the call's begins anew (a wave takes all of a page's new tokens: pages are meant to be of some hundred at most).  Values are the cache's (with SWA_KV_INT8 code times scale in fp32, rounded to dtype); what is no number stays
- *   in them.  The rows of one page follow each other in `slot` (as swa_paged_plan makes them).  The same call again gives the same bounds.
+ *   (offset 0) is among the call's begins anew (a wave takes all of a page's new tokens: pages are meant to be of some hundred at most).
+ *   Values are the cache's (with SWA_KV_INT8 code times scale in fp32, rounded to dtype); what is no number stays in them.  The rows of one
+ *   page follow each other in `slot` (as swa_paged_plan makes them).  The same call again gives the same bounds.
  *   A slot outside the pool is left out and sets the SWA_ERR_BAD_REQUEST bit.
  *   slot [n_rows], k_pages, k_scale (in); bounds [n_pages, h_kv, 2, d] dtype (in/out), 16-byte aligned.
  */
