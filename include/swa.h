@@ -635,9 +635,8 @@ int swa_paged_decode_selected(const swa_paged_params *params, swa_rows q, int32_
  *   out[r] = softmax over the tokens of both times their values, lse likewise; r, row_start, slot and skipped sequences as in swa_paged_decode_selected.
  * One prefix counts: prefix_of[prefix_of[s]] is not looked at.  Sequences whose prefix is none (outside 0..b-1, s itself, or an unused row with a negative
  * cache_len) are skipped and set the SWA_ERR_BAD_REQUEST bit; those of a prefix that is longer than its table or a stated len_bound are skipped and set the
- * SWA_ERR_CAPACITY bit.  params->window is 0.  Roundings as in swa_paged_decode, but for a prefix's weights where (b - 1) * h_q / h_kv is above 32 with 16-bit pages of
- * a multiple of eight tokens: these are rounded once to dtype (in fp16 in steps of 2^-35 of the largest, or finer).  A sequence's results may differ in their last bits with
- * the call's others, whose lengths and prefixes say where tokens are cut into pieces.
+ * SWA_ERR_CAPACITY bit.  params->window is 0.  Roundings as in swa_paged_decode.  A sequence's results may differ in their last bits with the call's others, whose
+ * lengths and prefixes say where tokens are cut into pieces.
  * SWA_ERR_CAPACITY also for more than a launch holds: 2^24 of b * h_q, and about 2^31 of h_kv * (2 b + b * h_q / h_kv / 32) * len / 128 with len the
  * longest sequence (of its table, len_bound).
  *   prefix_of [b] int32 (in).

@@ -384,16 +384,17 @@ __global__ void __launch_bounds__(256, Elem<C>::kBytes * D == 512 && ROWS == 2 ?
 // units for another).  Measured and no faster: the halves in turns, one forming products while the other forms weights (102); more tiles' fragments ahead; three parts of the
 // tokens.
 //
-// Weights are rounded once to the cache's type here.  Two numbers for a weight, as in the decode, are half as many products again and take 131 us instead of 100 (64 sequences
-// behind 8192 tokens, with up to 1024 of their own: 107 instead of 103); the error against 64 bits is 1.3 to 1.4 times that of weights in 32 bits, whose outputs are
-// rounded to the same type.  In fp16 weights are raised by 2^11: the largest is below 2^15, one of 2^-25 of it a normal number still.
+// Weights go to the second product as two numbers, as in the other forms, so that what a sequence gets does not hang on how many others its cache has room for: rounded once
+// they left outputs 1.3 to 1.4 times as far from 64 bits.  That is half as many products again.  Both are rounded to the nearest (split8), so an infinite value's product is
+// none; a unit with such a result is done again by the other form of the work.
 
 // The 16 weights of one lane's column, exp2(c scale - m), their sum, and the rescaling that goes with them: formed with the reference m as it is, and again where that turns out
-// too low (a sum above 2^15, or not finite, as on the first tile).
+// too low: in bf16 by a sum above 2^15 (or not finite, as on the first tile); in fp16, where the loudest weight is 2^15 (kRaise of the tiles), by one that is no fp16 number.
 template <typename T, int CT>
 __device__ __forceinline__ float column_weights(const float16_t& c, float scale, float& m, float& l, float16_t (&o)[CT], float (&p)[16])
 {
-    constexpr float kRaise = std::is_same_v<T, F16> ? 11.f : 0.f;
+    constexpr bool kHalf = std::is_same_v<T, F16>;
+    constexpr float kRaise = PagedTile<T, T, 32 * CT, 1>::kRaise;
     float sum;
     auto weights = [&]() __attribute__((always_inline)) {
         sum = 0.f;
@@ -404,7 +405,13 @@ __device__ __forceinline__ float column_weights(const float16_t& c, float scale,
         }
     };
     weights();
-    if (__any(sum > 32768.f)) {
+    float loudest = sum;
+    if constexpr (kHalf) {
+        loudest = p[0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) loudest = fmaxf(loudest, p[i]);
+    }
+    if (__any(loudest > (kHalf ? 65504.f : 32768.f))) {
         float most = c[0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) most = fmaxf(most, c[i]);
@@ -430,7 +437,8 @@ constexpr int wide_tile_bytes() { return 32 * D * 2; }
 template <int D>
 constexpr int wide_lds_bytes() { return 12 * wide_tile_bytes<D>() > kWideColumns * (D + 6) * 4 ? 12 * wide_tile_bytes<D>() : kWideColumns * (D + 6) * 4; }
 
-// Tokens begin .. end - 1 (begin a multiple of 32) for up to 128 columns.  False, and nothing is written: a page lies outside the pool (the first one stood in for it).
+// Tokens begin .. end - 1 (begin a multiple of 32) for up to 128 columns.  False, and nothing is written: a page lies outside the pool (the first one stood in for it), or a result
+// is not finite.
 template <typename T, int D, typename Q>
 __device__ __forceinline__ bool wide_part(const SharedArgs& a, const int32_t* table, int kv, int begin, int end, int columns, char* lds, Q from, int64_t to)
 {
@@ -543,7 +551,9 @@ __device__ __forceinline__ bool wide_part(const SharedArgs& a, const int32_t* ta
         float p[16];
         const float sum = column_weights<T>(c, a.pool.scale, m, l, o, p);
         l += sum;
-        const Vec16 pv[2] = {pack<T>(p), pack<T>(p + 8)};
+        Vec16 pv[2], rest[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) split8<T, true>(p + 8 * i, pv[i], rest[i]);
         auto vfrag = [&](int f) {
             const char* const at = sv + ((va ^ (f % CT << 6)) + f / CT * 16 * kRow);
             return lds_read_tr(at, at + 8 * kRow);
@@ -556,6 +566,7 @@ __device__ __forceinline__ bool wide_part(const SharedArgs& a, const int32_t* ta
             if (f + PF < 2 * CT) vf[f + PF] = vfrag(f + PF);
             __builtin_amdgcn_sched_barrier(0);
             o[f % CT] = Mfma<T>::run(vf[f], pv[f / CT], o[f % CT]);
+            o[f % CT] = Mfma<T>::run(vf[f], rest[f / CT], o[f % CT]);
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -591,7 +602,12 @@ __device__ __forceinline__ bool wide_part(const SharedArgs& a, const int32_t* ta
     float lo, hi;
     both_halves(l, lo, hi);
     l = lo + hi;
-    if (__syncthreads_or(bad)) return false;
+    float none = 0.f;
+#pragma unroll
+    for (int t = 0; t < CT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) none = __builtin_fmaf(o[t][i], 0.f, none);
+    if (__syncthreads_or(bad || none != none)) return false;
 
     // The second half's results to the first's, and from there to memory, whole rows at a time.
     constexpr int kPitch = D + 4;
@@ -637,7 +653,7 @@ __global__ void __launch_bounds__(512, 2) swa_paged_shared_wide_kernel(SharedArg
         a, SharedLists(reinterpret_cast<int*>(lds + wide_lds_bytes<D>()), a.b, scratch), member_row,
         [&](const int32_t* table, int kv, int begin, int end, int columns, auto from, int64_t to) __attribute__((always_inline)) {
             if (wide_part<T, D>(a, table, kv, begin, end, columns, lds, from, to)) return;
-            // (what a page outside the pool would hold is left out of the sums, which the other form of the work looks after)
+            // (the other form of the work leaves what a page outside the pool would hold out of the sums, and keeps infinite values)
             for (int c = 0; c < columns; c += 16)
                 shared_part<T, T, D, 1, 8, false>(a, table, kv, begin, end, columns - c < 16 ? columns - c : 16, sums, [&](int i) __attribute__((always_inline)) { return from(c + i); },
                                            SharedEmit<D>{a.part_out, a.part_sum, to + c});

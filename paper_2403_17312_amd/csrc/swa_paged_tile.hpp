@@ -41,14 +41,14 @@ __device__ __forceinline__ uint32_t round2(float lo, float hi)
 }
 
 // Eight weights (0 or more) as two numbers of the matrix cores' type each, big and rest.
-//   CODES: rounded to the nearest both times.
+//   FINITE (codes, or infinite results are looked after): rounded to the nearest both times.
 //   else: the values may be infinite, and a weight's two numbers have to be 0 or of its sign for an infinity to stay one.  So big is cut off, from what lies just below the
 //   weight (bf16), or rest is raised to fp16's smallest number (2^-39 of the largest weight; not for a weight of 0).
-template <typename P, bool CODES>
+template <typename P, bool FINITE>
 __device__ __forceinline__ void split8(const float* w, Vec16& big, Vec16& rest)
 {
     float f[8], r[8];
-    if constexpr (CODES) {
+    if constexpr (FINITE) {
         big = Vec16{round2<P>(w[0], w[1]), round2<P>(w[2], w[3]), round2<P>(w[4], w[5]), round2<P>(w[6], w[7])};
     } else if constexpr (std::is_same_v<P, F16>) {
         auto cut = [&](int i) { return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_pkrtz(w[i], w[i + 1])); };
@@ -62,7 +62,7 @@ __device__ __forceinline__ void split8(const float* w, Vec16& big, Vec16& rest)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         r[i] = w[i] - f[i];
-        if constexpr (!CODES && std::is_same_v<P, F16>) r[i] = fmaxf(r[i], fminf(w[i], 0x1p-24f));
+        if constexpr (!FINITE && std::is_same_v<P, F16>) r[i] = fmaxf(r[i], fminf(w[i], 0x1p-24f));
     }
     rest = Vec16{round2<P>(r[0], r[1]), round2<P>(r[2], r[3]), round2<P>(r[4], r[5]), round2<P>(r[6], r[7])};
 }
