@@ -548,7 +548,7 @@ int swa_paged_append(const swa_paged_params *params, swa_rows q, swa_rows k, swa
  * rows, or with a row beyond n_rows are skipped: nothing is written for them.  Where no token is left or every logit is -inf (so
  * for cache_len = 0), out = 0 and lse = -inf.
  * Accumulated in fp32; for their product with the values the weights are rounded to 15 bits in bf16, 21 in fp16 (2^-39 of the largest at the
- * least), 16 over 8-bit codes; out is rounded once.  A call's results do not depend on the order in which its workgroups run; a sequence's may differ
+ * least), 16 over 8-bit codes; out is rounded once.  An infinite value stays infinite where its weight is 2^-126 of the largest or more.  A call's results do not depend on the order in which its workgroups run; a sequence's may differ
  * in their last bits with the call's other lengths and with len_bound, which say where its tokens are cut into pieces.
  * A sequence that the plan refused keeps its rows in row_start and its cache_len: this call attends for it with whatever q holds
  * there, which swa_paged_append has not written.  swa_paged_decode_planned leaves such sequences out.

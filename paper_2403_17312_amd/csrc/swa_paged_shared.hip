@@ -389,12 +389,12 @@ __global__ void __launch_bounds__(256, Elem<C>::kBytes * D == 512 && ROWS == 2 ?
 // none; a unit with such a result is done again by the other form of the work.
 
 // The 16 weights of one lane's column, exp2(c scale - m), their sum, and the rescaling that goes with them: formed with the reference m as it is, and again where that turns out
-// too low: in bf16 by a sum above 2^15 (or not finite, as on the first tile); in fp16, where the loudest weight is 2^15 (kRaise of the tiles), by one that is no fp16 number.
+// too low: in bf16 by a sum above 2^15 (or not finite, as on the first tile); in fp16, where the loudest weight is 2^15, by one that is no fp16 number.
 template <typename T, int CT>
 __device__ __forceinline__ float column_weights(const float16_t& c, float scale, float& m, float& l, float16_t (&o)[CT], float (&p)[16])
 {
     constexpr bool kHalf = std::is_same_v<T, F16>;
-    constexpr float kRaise = PagedTile<T, T, 32 * CT, 1>::kRaise;
+    constexpr float kRaise = kHalf ? 15.f : 0.f;
     float sum;
     auto weights = [&]() __attribute__((always_inline)) {
         sum = 0.f;

@@ -42,11 +42,12 @@ __device__ __forceinline__ uint32_t round2(float lo, float hi)
 
 // Eight weights (0 or more) as two numbers of the matrix cores' type each, big and rest.
 //   FINITE (codes, or infinite results are looked after): rounded to the nearest both times.
-//   else: the values may be infinite, and a weight's two numbers have to be 0 or of its sign for an infinity to stay one.  So big is cut off, from what lies just below the
-//   weight (bf16), or rest is raised to fp16's smallest number (2^-39 of the largest weight; not for a weight of 0).
+//   else: the values may be infinite, and both of a weight's numbers have to be of its sign for an infinity to stay one.  So big is cut off, from what lies just below the
+//   weight (bf16), or both are raised to fp16's smallest number, 2^-40 of the largest weight, however small the weight is (but for 0).
 template <typename P, bool FINITE>
 __device__ __forceinline__ void split8(const float* w, Vec16& big, Vec16& rest)
 {
+    constexpr uint32_t kHighHalves = 0x07060302u;
     float f[8], r[8];
     if constexpr (FINITE) {
         big = Vec16{round2<P>(w[0], w[1]), round2<P>(w[2], w[3]), round2<P>(w[4], w[5]), round2<P>(w[6], w[7])};
@@ -55,16 +56,25 @@ __device__ __forceinline__ void split8(const float* w, Vec16& big, Vec16& rest)
         big = Vec16{cut(0), cut(2), cut(4), cut(6)};
     } else {
         auto below = [&](int i) { return __builtin_elementwise_sub_sat(f2u(w[i]), 1u); };
-        auto cut = [&](int i) { return __builtin_amdgcn_perm(below(i + 1), below(i), 0x07060302u); };
+        auto cut = [&](int i) { return __builtin_amdgcn_perm(below(i + 1), below(i), kHighHalves); };
         big = Vec16{cut(0), cut(2), cut(4), cut(6)};
     }
     unpack<P>(big, f);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        r[i] = w[i] - f[i];
-        if constexpr (!FINITE && std::is_same_v<P, F16>) r[i] = fmaxf(r[i], fminf(w[i], 0x1p-24f));
-    }
+    for (int i = 0; i < 8; ++i) r[i] = w[i] - f[i];
     rest = Vec16{round2<P>(r[0], r[1]), round2<P>(r[2], r[3]), round2<P>(r[4], r[5]), round2<P>(r[6], r[7])};
+    if constexpr (!FINITE && std::is_same_v<P, F16>) {
+        typedef uint16_t halves_t __attribute__((ext_vector_type(2)));
+        auto raise = [&](int i, uint32_t& a, uint32_t& b) {         // (as whole numbers, of which 1 is the smallest fp16 one)
+            const halves_t least = __builtin_elementwise_min(__builtin_bit_cast(halves_t, __builtin_amdgcn_perm(f2u(w[i + 1]), f2u(w[i]), kHighHalves)), halves_t{1, 1});
+            a = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(halves_t, a), least));
+            b = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(halves_t, b), least));
+        };
+        raise(0, big.x, rest.x);
+        raise(2, big.y, rest.y);
+        raise(4, big.z, rest.z);
+        raise(6, big.w, rest.w);
+    }
 }
 
 template <typename V>
@@ -87,10 +97,10 @@ struct PagedTile {
     static constexpr int kTiles = kWide && (D == 128 || ROWS == 2) ? 1 : 2, kKeys = 16 * kTiles, kRow = D * Elem<C>::kBytes;
     static constexpr int kSteps = kWide ? D / 16 : D / 32;       // operands of a logit
     static constexpr int kChannels = D / 16;                     // of V in a lane
-    // A weight is exp2(x - top + kRaise).  fp16 has 2^-14 to 2^15 for normal numbers: raised so far the largest weight is 2^15 and half a step of
+    // A weight is exp2(x - top + kRaise).  fp16 has 2^-14 to 2^16 for normal numbers: raised so far the largest weight is 2^16 (65504, and a rest of 32) and a step of
     // the smallest numbers 2^-40 of it.  Without, a wave lost what lies 17.4 nats below its loudest token, which for 131072 such tokens beside one
     // of small value was 6.7 % of the output.  The sum carries the same factor, so nothing takes it back but the maximum, as it is handed on.
-    static constexpr float kRaise = std::is_same_v<C, F16> ? 15.f : 0.f;
+    static constexpr float kRaise = std::is_same_v<C, F16> ? 16.f : 0.f;
     static constexpr int kLoads = kCodes ? D / 64 : kSteps, kVLoad = kWide ? D / 64 : 1, kVBytes = kWide ? 16 : kChannels * Elem<C>::kBytes;
     struct alignas(kVBytes < 16 ? kVBytes : 16) Values { uint32_t w[kVBytes / 4]; };
     // Where in a query row operand c of lanes `j` begins, in bytes (16 bytes of codes are two operands' channels).
