@@ -637,8 +637,8 @@ int swa_paged_decode_selected(const swa_paged_params *params, swa_rows q, int32_
  * cache_len) are skipped and set the SWA_ERR_BAD_REQUEST bit; those of a prefix that is longer than its table or a stated len_bound are skipped and set the
  * SWA_ERR_CAPACITY bit.  params->window is 0.  Roundings as in swa_paged_decode.  A sequence's results may differ in their last bits with the call's others, whose
  * lengths and prefixes say where tokens are cut into pieces.
- * SWA_ERR_CAPACITY also for more than a launch holds: 2^24 of b * h_q, and about 2^31 of h_kv * (2 b + b * h_q / h_kv / 32) * len / 128 with len the
- * longest sequence (of its table, len_bound).
+ * SWA_ERR_CAPACITY also for more than a launch holds: 2^24 of b * h_q; and 2^31 of h_kv * (b + b * h_q / h_kv / columns) * len / 128, each quotient rounded up, with len the longest
+ * sequence (of its table, len_bound) and columns 128 or 32, where (b - 1) * h_q / h_kv is up to 16 these (one sequence: never).
  *   prefix_of [b] int32 (in).
  */
 int swa_paged_decode_shared(const swa_paged_params *params, swa_rows q, int32_t n_rows, const int32_t *row_start, const int32_t *slot,

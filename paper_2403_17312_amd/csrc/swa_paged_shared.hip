@@ -37,15 +37,16 @@ struct SharedArgs {
     uint32_t page_mul;                             // t / page_size = t * page_mul >> page_shift for 0 <= t < 2^31
     int32_t page_shift;
     int32_t sixteens;                              // pages are whole sixteens of tokens
+    int32_t own_log;                               // tokens of a sequence's own step, as a power of two
 };
 
 constexpr int kNoPrefix = 0, kLeftOut = 0xffff;    // of a sequence, where it has no prefix or the call leaves it out; else the prefix's number and 1
 
 __device__ __forceinline__ int steps_of(int tokens) { return (tokens + kPagedStep - 1) / kPagedStep; }
 
-// A sequence's own tokens: steps of 32, and one that stands for what a unit costs before its first key.
-constexpr int kOwnStep = 32, kOwnColumns = 16;
-__device__ __forceinline__ int own_steps_of(int tokens) { return tokens > 0 ? 1 + (tokens + kOwnStep - 1) / kOwnStep : 0; }
+// A sequence's own tokens: steps of 32 (of more where a call could have 2^31 of them), and one that stands for what a unit costs before its first key.
+constexpr int kOwnLog = 5, kOwnColumns = 16;
+__host__ __device__ __forceinline__ int own_steps_of(int tokens, int log) { return tokens > 0 ? 1 + ((tokens - 1) >> log) + 1 : 0; }
 
 // A partial result, by sixteen threads.
 template <int D>
@@ -236,7 +237,7 @@ __device__ __forceinline__ void shared_share(const SharedArgs& a, const SharedLi
                 else if (m > a.rows.len_max) bits |= kStatusCapacityBit;
                 is = m < 0 || m > a.rows.len_max ? kLeftOut : of + 1;
             }
-            if (is != kLeftOut) steps = own_steps_of(n) * own_tiles;
+            if (is != kLeftOut) steps = own_steps_of(n, a.own_log) * own_tiles;
             if (is != kLeftOut && is != kNoPrefix) atomicAdd(&before[1 + of], 1);
         }
         if (too_long) bits |= kStatusCapacityBit;
@@ -344,7 +345,7 @@ __device__ __forceinline__ void shared_share(const SharedArgs& a, const SharedLi
             const int last = steps - first < x1 - x ? steps : first + (x1 - x);
             if (last > 1) {                              // (a unit's first step has no tokens)
                 const int row = row_of(s), n = __builtin_amdgcn_readfirstlane(a.rows.cache_len[s]);
-                const int begin = first ? (first - 1) * kOwnStep : 0, end = last == steps ? n : (last - 1) * kOwnStep,
+                const int begin = first ? (first - 1) << a.own_log : 0, end = last == steps ? n : (last - 1) << a.own_log,
                           here = a.group - tile * kOwnColumns < kOwnColumns ? a.group - tile * kOwnColumns : kOwnColumns;
                 own_part<T, C, D>(a, a.block_table + (int64_t)s * a.max_pages, kv, begin, end, here,
                                   a.q + row * a.q_stride + ((int64_t)kv * a.group + tile * kOwnColumns) * (D * Elem<T>::kBytes),
@@ -791,10 +792,11 @@ int launch_paged_shared(const swa_paged_params& p, const swa_rows& q, int32_t n_
     const bool again = most_columns(p) > 32;             // a prefix may have several units a key head
     a.shares = shared_shares(rows);
     a.own_columns = prefix_columns(p);
-    // (steps are 32-bit numbers: of every sequence's own tokens, and of as many prefixes as may be)
+    // (steps are 32-bit numbers: of as many prefixes as may be, and of every sequence's own tokens, whose steps grow until they are)
     const int64_t own_units = (int64_t)p.b * ((a.group + kOwnColumns - 1) / kOwnColumns) * p.h_kv,
-                  units = (((int64_t)p.b * a.group + 16 * rows - 1) / (16 * rows) + p.b) * p.h_kv, steps = ((int64_t)a.rows.len_max + kPagedStep - 1) / kPagedStep;
-    if (units > 0x7fffffffLL / steps || own_units > 0x7fffffffLL / (4 * steps + 1) || (uint64_t)p.b * p.h_q * 256 > 0xffffffffULL) return SWA_ERR_CAPACITY;
+                  units = p.b > 1 ? (((int64_t)p.b * a.group + 16 * rows - 1) / (16 * rows) + p.b) * p.h_kv : 0, steps = ((int64_t)a.rows.len_max + kPagedStep - 1) / kPagedStep;
+    if (units > 0x7fffffffLL / steps || (uint64_t)p.b * p.h_q * 256 > 0xffffffffULL) return SWA_ERR_CAPACITY;
+    for (a.own_log = kOwnLog; own_units > 0x7fffffffLL / own_steps_of(a.rows.len_max, a.own_log); ++a.own_log) {}
 #define SWA_SHARED(T, C) (p.d == 64 ? launch_shared_form<T, C, 64>(a, rows, again, stream) : launch_shared_form<T, C, 128>(a, rows, again, stream))
     const int rc = p.dtype == SWA_F32   ? SWA_SHARED(F32, F32)
                    : p.dtype == SWA_F16 ? (paged_int8(p) ? SWA_SHARED(F16, Q8) : SWA_SHARED(F16, F16))

@@ -131,3 +131,25 @@ def test_the_lists_of_all_sequences_fit_in_lds(B, kernels):  # noqa: F811
             seen += 1
             assert lds <= 36 * 1024 and lds + 4 * (2 * B.SWA_MAX_PAGED_SEQS + 1) + 2 * (2 * B.SWA_MAX_PAGED_SEQS + 2) <= 160 * 1024, k
     assert seen
+
+
+# (a call that is not refused goes to the device: only where there is none)
+@pytest.mark.skipif(torch.cuda.is_available(), reason="the tensors are none")
+@pytest.mark.parametrize("b,h_q,h_kv,tokens,more", [
+    (2048, 128, 8, 1 << 22, {}), (256, 136, 8, 1 << 24, {}), (64, 1024, 8, 1 << 26, {}), (1, 4096, 32, 1 << 30, {}), (1, 65535, 65535, 1 << 30, {}),
+    (2, 40, 5, 1 << 30, {}), (4, 5, 1, 1 << 30, {}), (16, 64, 4, 1 << 29, dict(dtype=0)), (4096, 4095, 1, 1 << 18, {}), (17, 8, 8, 1 << 30, dict(len_bound=1 << 29)),
+])
+def test_sizes_that_a_launch_holds(B, b, h_q, h_kv, tokens, more):  # noqa: F811
+    """Just below the limit that the header states, which a call twice as long (or wide) passes."""
+    p = params(B, b=b, h_q=h_q, h_kv=h_kv, page_size=4096, n_pages=1, max_pages=tokens // 4096, **more)
+    assert shared(B, p, n=b, q=B.SwaRows(ok, h_q * p.d)) not in (B.SWA_ERR_CAPACITY, B.SWA_OK)
+
+
+@pytest.mark.parametrize("b,h_q,h_kv,page,tokens,more", [
+    (2048, 128, 8, 4096, 1 << 24, {}), (256, 136, 8, 4096, 1 << 27, {}), (256, 136, 8, 4092, 1023 * 4092 * 60, {}), (64, 1024, 8, 4096, 1 << 29, {}), (256, 8, 8, 4096, 1 << 30, {}),
+    (2, 1 << 15, 128, 4096, 1 << 30, dict(dtype=0)), (4096, 4096, 1, 4096, 4096, {}),
+])
+def test_sizes_that_no_launch_holds(B, b, h_q, h_kv, page, tokens, more):  # noqa: F811
+    """Just beyond it."""
+    p = params(B, b=b, h_q=h_q, h_kv=h_kv, page_size=page, n_pages=1, max_pages=tokens // page, **more)
+    assert shared(B, p, n=b, q=B.SwaRows(ok, h_q * p.d)) == B.SWA_ERR_CAPACITY
