@@ -595,7 +595,8 @@ int swa_paged_bounds(const swa_paged_params *params, int32_t n_rows, const int32
 
 /*
  * score[s][h][j] = max over the query heads of key head h of scale * sum_c (max(q_c, 0) * hi_c + min(q_c, 0) * lo_c), for the pages j of sequence s that hold
- * tokens: at least every logit of the page's keys (with SWA_KV_INT8: of keys rounded to dtype).  Accumulated in fp32.  What is no number (a key or query
+ * tokens: at least every logit of the page's keys.  With SWA_KV_INT8 the bounds are rounded ones, and scale * sum_c |q_c| e_c is added, with e_c the half step of dtype at the bound that
+ * the term has (2^-11 of it in fp16, 2^-8 in bf16, and a 4096th more).  Accumulated in fp32.  What is no number (a key or query
  * that is not finite) scores +inf, a page outside the pool -inf, and sets the SWA_ERR_BAD_REQUEST bit.  Other entries are left as they were.
  * Sequences are left out as by the attention; one longer than its table or a stated len_bound sets the SWA_ERR_CAPACITY bit.
  * SWA_ERR_CAPACITY also where b * h_kv times the pages that a sequence may have reaches 2^31.

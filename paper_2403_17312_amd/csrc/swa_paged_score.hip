@@ -20,7 +20,7 @@ struct ScoreArgs {
     int32_t group, ranges, log_heads;              // query heads of a key head; shares, or workgroups of a sequence; key heads of an item
     uint32_t group_mul;                            // t / group = t * group_mul >> group_shift
     int32_t group_shift;
-    float scale;
+    float scale, half_step;                        // of logits; what rounding may have moved a bound by, relative to it (codes)
 };
 
 // Waves of a workgroup, of which each has sixteen rows in LDS.
@@ -42,8 +42,22 @@ __device__ __forceinline__ Vec16 part_of(const Vec16& v, bool negative)
     return Vec16{word(v.x), word(v.y), word(v.z), word(v.w)};
 }
 
-// WHOLE: a load takes rows of one page.  SHARES: the items of all sequences are laid end to end and cut evenly, which every workgroup does by itself; else `ranges` workgroups serve one sequence.
-template <typename T, int D, bool WHOLE, bool SHARES>
+// Sizes of 16-bit bounds, at least the smallest normal number, below which steps get no smaller.
+template <typename T>
+__device__ __forceinline__ Vec16 sizes_of(const Vec16& v)
+{
+    typedef uint16_t halves_t __attribute__((ext_vector_type(2)));
+    constexpr uint16_t kLeast = std::is_same_v<T, F16> ? 0x0400 : 0x0080;
+    auto word = [&](uint32_t w) {
+        return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(halves_t, w & 0x7fff7fffu), halves_t{kLeast, kLeast}));
+    };
+    return Vec16{word(v.x), word(v.y), word(v.z), word(v.w)};
+}
+__device__ __forceinline__ Vec16 positive(const Vec16& v) { return Vec16{v.x & 0x7fff7fffu, v.y & 0x7fff7fffu, v.z & 0x7fff7fffu, v.w & 0x7fff7fffu}; }
+
+// CODES: bounds of codes are the rounded ones, and half a step of each goes on top: sum_c |q_c| |bound_c| by the matrix cores, too (the 51 us
+// above are 52.4, and 8 short sequences 5.47 instead of 5.28).  WHOLE: a load takes rows of one page.  SHARES: the items of all sequences are laid end to end and cut evenly, which every workgroup does by itself; else `ranges` workgroups serve one sequence.
+template <typename T, int D, bool CODES, bool WHOLE, bool SHARES>
 __global__ void __launch_bounds__(64 * score_waves(2 * D * Elem<T>::kBytes)) swa_paged_score_kernel(ScoreArgs a)
 {
     constexpr int kHalf = D * Elem<T>::kBytes, kRow = 2 * kHalf, kSteps = kHalf / 64, kLoads = 2 * kSteps, kChunks = kRow / 16, kRows = 64 / kChunks,
@@ -170,6 +184,14 @@ __global__ void __launch_bounds__(64 * score_waves(2 * D * Elem<T>::kBytes)) swa
         for (int c0 = 0;;) {
             const int of = (int)(((uint64_t)(uint32_t)(c0 + col) * a.group_mul) >> a.group_shift);     // the key head of this lane's column
             f32x4_t sum = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (CODES) {
+#pragma unroll
+                for (int c = 0; c < kSteps; ++c) {
+                    sum = mfma16<T>(sizes_of<T>(box[c]), positive(part_of<T>(q[c], true)), sum);
+                    sum = mfma16<T>(sizes_of<T>(box[kSteps + c]), part_of<T>(q[c], false), sum);
+                }
+                sum *= a.half_step;
+            }
 #pragma unroll
             for (int c = 0; c < kSteps; ++c) {
                 sum = mfma16<T>(box[c], part_of<T>(q[c], true), sum);
@@ -218,6 +240,7 @@ int launch_paged_score(const swa_paged_params& p, const swa_rows& q, int32_t n_r
     a.max_pages = p.max_pages;
     a.group = p.h_q / p.h_kv;
     a.scale = p.scale > 0.f ? p.scale : 1.f / sqrtf((float)p.d);
+    a.half_step = (p.dtype == SWA_F16 ? 0x1p-11f : 0x1p-8f) * (1.f + 0x1p-12f);       // (the second factor for code times scale in fp32)
     page_divisor(a.group, a.group_mul, a.group_shift);
     // As many key heads to an item as there are columns for: a page's rows of them lie behind each other.
     a.log_heads = 3;
@@ -237,13 +260,13 @@ int launch_paged_score(const swa_paged_params& p, const swa_rows& q, int32_t n_r
     const dim3 grid((unsigned)(in_shares ? ranges : p.b * ranges)), block(64 * waves);
     const size_t lds = in_shares ? sizeof(int) * ((size_t)p.b + 1) : 0;
     const bool whole = (row_bytes << a.log_heads) >= 1024;
-#define SWA_SCORE_FORM(T, D, W) (in_shares ? launch_kernel(swa_paged_score_kernel<T, D, W, true>, grid, block, lds, stream, a) \
-                                           : launch_kernel(swa_paged_score_kernel<T, D, W, false>, grid, block, lds, stream, a))
-#define SWA_SCORE(T) (p.d == 64 ? (whole ? SWA_SCORE_FORM(T, 64, true) : SWA_SCORE_FORM(T, 64, false)) \
-                                : (whole ? SWA_SCORE_FORM(T, 128, true) : SWA_SCORE_FORM(T, 128, false)))
-    if (p.dtype == SWA_F32) SWA_SCORE(F32);
-    else if (p.dtype == SWA_F16) SWA_SCORE(F16);
-    else SWA_SCORE(BF16);
+#define SWA_SCORE_FORM(T, D, C, W) (in_shares ? launch_kernel(swa_paged_score_kernel<T, D, C, W, true>, grid, block, lds, stream, a) \
+                                              : launch_kernel(swa_paged_score_kernel<T, D, C, W, false>, grid, block, lds, stream, a))
+#define SWA_SCORE(T, C) (p.d == 64 ? (whole ? SWA_SCORE_FORM(T, 64, C, true) : SWA_SCORE_FORM(T, 64, C, false)) \
+                                   : (whole ? SWA_SCORE_FORM(T, 128, C, true) : SWA_SCORE_FORM(T, 128, C, false)))
+    if (p.dtype == SWA_F32) SWA_SCORE(F32, false);
+    else if (p.dtype == SWA_F16) paged_int8(p) ? SWA_SCORE(F16, true) : SWA_SCORE(F16, false);
+    else paged_int8(p) ? SWA_SCORE(BF16, true) : SWA_SCORE(BF16, false);
 #undef SWA_SCORE
 #undef SWA_SCORE_FORM
     return hipGetLastError() == hipSuccess ? SWA_OK : SWA_ERR_HIP;
