@@ -488,7 +488,8 @@ typedef struct {
 } swa_rows;
 
 /* Workspace of the paged calls, as swa_workspace_bytes, swa_workspace_init and swa_check_status are for the others.  The size
- * goes by b, the heads, d and dtype.  Calls that overlap in time need workspaces of their own. */
+ * goes by b, the heads, d and dtype; for two sequences and more it is mostly what swa_paged_decode_shared asks for.  Calls that
+ * overlap in time need workspaces of their own. */
 size_t swa_paged_workspace_bytes(const swa_paged_params *params);
 int swa_paged_workspace_init(const swa_paged_params *params, void *workspace, void *stream);
 int swa_paged_check_status(const swa_paged_params *params, void *workspace, void *stream, int32_t *status_out);
@@ -639,7 +640,8 @@ int swa_paged_decode_selected(const swa_paged_params *params, swa_rows q, int32_
  * SWA_ERR_CAPACITY bit.  params->window is 0.  Roundings as in swa_paged_decode.  A sequence's results may differ in their last bits with the call's others, whose
  * lengths and prefixes say where tokens are cut into pieces.
  * SWA_ERR_CAPACITY also for more than a launch holds: 2^24 of b * h_q; and 2^31 of h_kv * (b + b * h_q / h_kv / columns) * len / 128, each quotient rounded up, with len the longest
- * sequence (of its table, len_bound) and columns 128 or 32, where (b - 1) * h_q / h_kv is up to 16 these (one sequence: never).
+ * sequence (of its table, len_bound) and columns 128 or 32, where (b - 1) * h_q / h_kv is up to 16 these
+ * (one sequence: as swa_paged_decode).
  *   prefix_of [b] int32 (in).
  */
 int swa_paged_decode_shared(const swa_paged_params *params, swa_rows q, int32_t n_rows, const int32_t *row_start, const int32_t *slot,

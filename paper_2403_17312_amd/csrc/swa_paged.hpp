@@ -33,7 +33,8 @@ inline int32_t paged_len_max(const swa_paged_params& p)
 }
 inline int32_t paged_pages_max(const swa_paged_params& p) { return (int32_t)(((int64_t)paged_len_max(p) + p.page_size - 1) / p.page_size); }
 
-constexpr size_t kPagedPartialOffset = 256;    // the status word lies before the attention's partial results
+constexpr size_t kPagedPartialOffset = 256;    // the status word lies before the attention's partial results,
+constexpr size_t kPagedLengthOffset = 128;     // and the length that a single sequence of swa_paged_decode_shared has for the call
 
 // Query heads of a workgroup: the matrix cores' 16 columns, or twice as many, so that keys and values shared by more heads are read half as often.
 inline int tile_heads_of(const swa_paged_params& p) { return p.h_q / p.h_kv > 16 ? 32 : 16; }

@@ -692,6 +692,17 @@ __global__ void __launch_bounds__(256) swa_paged_join_shared_kernel(SharedArgs a
                             count + own_count, a.out, a.lse, (int64_t)at.row * a.h_q + hq);
 }
 
+// A single sequence has no other one for a prefix: its length, where it has none, or that of an unused row.
+__global__ void swa_paged_shared_alone_kernel(PagedRows rows, const int32_t* prefix_of, int32_t* len, int32_t* status)
+{
+    if (threadIdx.x) return;
+    int row, n;
+    bool too_long = false;
+    const bool refused = paged_row(rows, 0, row, n, too_long) && prefix_of[0] != -1;
+    if (refused) atomicOr(status, kStatusBadRequestBit);
+    *len = refused ? -1 : n;
+}
+
 // Columns that a prefix can have.
 static int64_t most_columns(const swa_paged_params& p) { return (int64_t)(p.b - 1) * (p.h_q / p.h_kv); }
 
@@ -711,6 +722,7 @@ static int64_t shared_columns(const swa_paged_params& p) { return prefix_columns
 
 size_t paged_shared_bytes(const swa_paged_params& p)
 {
+    if (p.b == 1) return 0;
     return (size_t)shared_columns(p) * (p.d + 2) * sizeof(float) + ((size_t)p.b + 1) * sizeof(SharedPlace);
 }
 
@@ -765,6 +777,13 @@ int launch_paged_shared(const swa_paged_params& p, const swa_rows& q, int32_t n_
                         const void* k_pages, const void* v_pages, const float* k_scale, const float* v_scale, const int32_t* block_table,
                         const int32_t* cache_len, const int32_t* prefix_of, void* out, float* lse, void* workspace, hipStream_t stream)
 {
+    if (p.b == 1) {                                      // the decode's, with its limit and its workspace
+        if (p.h_kv * (((int64_t)paged_len_max(p) + kPagedStep - 1) / kPagedStep) > 0x7fffffffLL) return SWA_ERR_CAPACITY;
+        int32_t* const len = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + kPagedLengthOffset);
+        launch_kernel(swa_paged_shared_alone_kernel, dim3(1), dim3(64), 0, stream, PagedRows{row_start, slot, cache_len, n_rows, paged_len_max(p)}, prefix_of, len,
+                      paged_status(workspace));
+        return launch_paged_decode(p, q, n_rows, row_start, slot, k_pages, v_pages, k_scale, v_scale, block_table, len, out, lse, workspace, stream);
+    }
     SharedArgs a{};
     a.q = static_cast<const char*>(q.data);
     a.q_stride = q.stride * (p.dtype == SWA_F32 ? 4 : 2);
@@ -794,7 +813,7 @@ int launch_paged_shared(const swa_paged_params& p, const swa_rows& q, int32_t n_
     a.own_columns = prefix_columns(p);
     // (steps are 32-bit numbers: of as many prefixes as may be, and of every sequence's own tokens, whose steps grow until they are)
     const int64_t own_units = (int64_t)p.b * ((a.group + kOwnColumns - 1) / kOwnColumns) * p.h_kv,
-                  units = p.b > 1 ? (((int64_t)p.b * a.group + 16 * rows - 1) / (16 * rows) + p.b) * p.h_kv : 0, steps = ((int64_t)a.rows.len_max + kPagedStep - 1) / kPagedStep;
+                  units = (((int64_t)p.b * a.group + 16 * rows - 1) / (16 * rows) + p.b) * p.h_kv, steps = ((int64_t)a.rows.len_max + kPagedStep - 1) / kPagedStep;
     if (units > 0x7fffffffLL / steps || (uint64_t)p.b * p.h_q * 256 > 0xffffffffULL) return SWA_ERR_CAPACITY;
     for (a.own_log = kOwnLog; own_units > 0x7fffffffLL / own_steps_of(a.rows.len_max, a.own_log); ++a.own_log) {}
 #define SWA_SHARED(T, C) (p.d == 64 ? launch_shared_form<T, C, 64>(a, rows, again, stream) : launch_shared_form<T, C, 128>(a, rows, again, stream))

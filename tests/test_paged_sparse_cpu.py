@@ -136,7 +136,7 @@ def test_the_lists_of_all_sequences_fit_in_lds(B, kernels):  # noqa: F811
 # (a call that is not refused goes to the device: only where there is none)
 @pytest.mark.skipif(torch.cuda.is_available(), reason="the tensors are none")
 @pytest.mark.parametrize("b,h_q,h_kv,tokens,more", [
-    (2048, 128, 8, 1 << 22, {}), (256, 136, 8, 1 << 24, {}), (64, 1024, 8, 1 << 26, {}), (1, 4096, 32, 1 << 30, {}), (1, 65535, 65535, 1 << 30, {}),
+    (2048, 128, 8, 1 << 22, {}), (256, 136, 8, 1 << 24, {}), (64, 1024, 8, 1 << 26, {}), (1, 4096, 32, 1 << 30, {}),
     (2, 40, 5, 1 << 30, {}), (4, 5, 1, 1 << 30, {}), (16, 64, 4, 1 << 29, dict(dtype=0)), (4096, 4095, 1, 1 << 18, {}), (17, 8, 8, 1 << 30, dict(len_bound=1 << 29)),
 ])
 def test_sizes_that_a_launch_holds(B, b, h_q, h_kv, tokens, more):  # noqa: F811
@@ -147,9 +147,17 @@ def test_sizes_that_a_launch_holds(B, b, h_q, h_kv, tokens, more):  # noqa: F811
 
 @pytest.mark.parametrize("b,h_q,h_kv,page,tokens,more", [
     (2048, 128, 8, 4096, 1 << 24, {}), (256, 136, 8, 4096, 1 << 27, {}), (256, 136, 8, 4092, 1023 * 4092 * 60, {}), (64, 1024, 8, 4096, 1 << 29, {}), (256, 8, 8, 4096, 1 << 30, {}),
-    (2, 1 << 15, 128, 4096, 1 << 30, dict(dtype=0)), (4096, 4096, 1, 4096, 4096, {}),
+    (2, 1 << 15, 128, 4096, 1 << 30, dict(dtype=0)), (4096, 4096, 1, 4096, 4096, {}), (1, 65535, 65535, 4096, 1 << 30, {}),
 ])
 def test_sizes_that_no_launch_holds(B, b, h_q, h_kv, page, tokens, more):  # noqa: F811
     """Just beyond it."""
     p = params(B, b=b, h_q=h_q, h_kv=h_kv, page_size=page, n_pages=1, max_pages=tokens // page, **more)
     assert shared(B, p, n=b, q=B.SwaRows(ok, h_q * p.d)) == B.SWA_ERR_CAPACITY
+
+
+def test_a_single_sequence_needs_no_room_for_prefixes(B):  # noqa: F811
+    """It has the decode's workspace: at most two pieces for each of 1024 shares, of 16 heads' sums and outputs."""
+    for h_q, h_kv, d, dtype in ((1, 1, 64, 1), (32, 8, 128, 2), (16, 16, 128, 0), (64, 8, 64, 1)):
+        n = B.swa_paged_workspace_bytes(params(B, b=1, h_q=h_q, h_kv=h_kv, d=d, dtype=dtype))
+        assert 256 < n <= 2 * 1024 * 16 * (d + 2) * 4 + 512
+        assert B.swa_paged_workspace_bytes(params(B, b=2, h_q=h_q, h_kv=h_kv, d=d, dtype=dtype)) > n
