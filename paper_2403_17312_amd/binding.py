@@ -644,11 +644,17 @@ class PagedCache:
     def _cache(self, layer: int):
         return self.k_pages[layer], self.v_pages[layer], self.k_scale[layer], self.v_scale[layer], self.block_table, self.cache_len
 
-    def decode_sparse(self, layer: int, q, out, first: int = 1, last: int = 2, lse=None, by_rows: bool = False, stream=None) -> None:
-        """decode() over `select` pages of each sequence and key head: the `first` first ones, the `last` last ones, and those whose bounds promise the largest
-        logits (score, sel and sel_cnt hold what was found, until the next call)."""
+    def decode_sparse(self, layer: int, q, out, first: int = None, last: int = None, lse=None, by_rows: bool = False, stream=None) -> None:
+        """decode() over `select` pages of each sequence and key head: the `first` first ones, the `last` last ones (unless said otherwise one and two, where so many are
+        selected; of fewer, the last ones), and those whose bounds promise the largest logits (score, sel and sel_cnt hold what was found, until the next call)."""
         if not self.select:
             raise ValueError("this cache keeps no bounds: PagedCache(..., select=...)")
+        if last is None:
+            last = min(2, max(self.select - (first or 0), 0))
+        if first is None:
+            first = min(1, max(self.select - last, 0))
+        if first < 0 or last < 0 or first + last > self.select:
+            raise ValueError(f"first and last are numbers of pages, {self.select} together at most; got {first} and {last}")
         n, rows, slot = self._queries(q, out, lse, by_rows)
         p, ws = self.params, self.workspace
         swa_paged_score(p, q, n, rows, slot, self.bounds[layer], self.block_table, self.cache_len, self.score, ws, stream)
