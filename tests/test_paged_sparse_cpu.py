@@ -161,3 +161,14 @@ def test_a_single_sequence_needs_no_room_for_prefixes(B):  # noqa: F811
         n = B.swa_paged_workspace_bytes(params(B, b=1, h_q=h_q, h_kv=h_kv, d=d, dtype=dtype))
         assert 256 < n <= 2 * 1024 * 16 * (d + 2) * 4 + 512
         assert B.swa_paged_workspace_bytes(params(B, b=2, h_q=h_q, h_kv=h_kv, d=d, dtype=dtype)) > n
+
+
+@pytest.mark.parametrize("t", ["3F16", "4BF16"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_lists_fit_beside_the_tiles_of_many_columns(B, kernels, t, d):  # noqa: F811
+    """Of which the launch takes 1 KiB for the kernel's own LDS, and twelve tiles of 32 rows or the results of 128 columns; and its loop spills nothing."""
+    seen = [k for k in kernels if "swa_paged_shared_wide_kernel" in k and f"INS_{t}ELi{d}EE" in k]
+    assert len(seen) == 1
+    tiles = max(12 * 32 * d * 2, 128 * (d + 6) * 4)
+    _, scratch, lds = kernels[seen[0]]
+    assert scratch == 0 and lds <= 1024 and lds + tiles + 4 * (2 * B.SWA_MAX_PAGED_SEQS + 2) + 2 * (2 * B.SWA_MAX_PAGED_SEQS + 1) + 15 <= 160 * 1024
