@@ -600,7 +600,7 @@ int swa_paged_bounds(const swa_paged_params *params, int32_t n_rows, const int32
  * the term has (2^-11 of it in fp16, 2^-8 in bf16, and a 4096th more).  Accumulated in fp32.  What is no number (a key or query
  * that is not finite) scores +inf, a page outside the pool -inf, and sets the SWA_ERR_BAD_REQUEST bit.  Other entries are left as they were.
  * Sequences are left out as by the attention; one longer than its table or a stated len_bound sets the SWA_ERR_CAPACITY bit.
- * SWA_ERR_CAPACITY also where b * h_kv times the pages that a sequence may have reaches 2^31.
+ * SWA_ERR_CAPACITY also where b * h_kv times the pages that a sequence may have reaches 2^31 - 2^16.
  *   q [n_rows, h_q, d], bounds, block_table, cache_len (in); score [b, h_kv, max_pages] float32 (out).
  */
 int swa_paged_score(const swa_paged_params *params, swa_rows q, int32_t n_rows, const int32_t *row_start, const int32_t *slot,
@@ -622,7 +622,7 @@ int swa_paged_select(const swa_paged_params *params, const float *score, const i
  * swa_paged_decode over the tokens of listed pages alone: those of pages sel[s][h][0 .. sel_cnt[s][h]) for the query heads of key head h.  lse is theirs, too.
  * Entries below zero, and those of pages without tokens, count for nothing; entries of max_pages and more, pages outside the pool and a sel_cnt outside
  * 0..n_sel (which counts as the nearer end) set the SWA_ERR_BAD_REQUEST bit.  A page listed twice counts twice.  Without tokens, out = 0 and lse = -inf.
- * Everything else is as there, the roundings and skipped sequences too; the launch goes by n_sel * page_size tokens, and b * h_q is below 2^24 (SWA_ERR_CAPACITY).
+ * Everything else is as there, the roundings and skipped sequences too; the launch goes by n_sel * page_size tokens, and b * h_q is below 2^24 - 7 (SWA_ERR_CAPACITY).
  */
 int swa_paged_decode_selected(const swa_paged_params *params, swa_rows q, int32_t n_rows, const int32_t *row_start, const int32_t *slot,
                               const void *k_pages, const void *v_pages, const float *k_scale, const float *v_scale,

@@ -3,7 +3,7 @@
 // The minimum of a page that grows is the minimum of what it was and of the new keys, so a call reads its new rows, and the old values of the pages that
 // had tokens before.  Bound: the launch for a step (64 sequences, 8 key heads of 128 bf16 channels, 3.5 us) and its chain of loads for prompts: slots, rows, the page's old
 // values.  A wave takes one key head of a page: the call's rows of that page follow each other in `slot`, the first of them finds the others, a load fetches as many whole rows
-// as the wave holds, and four loads are under way at once (9.5 MB of 8-bit codes, pages of 16: 7.3 us; one load at a time, and teams of lanes joined by way of LDS, 9.7).
+// as the wave holds, and four loads are under way at once (9.5 MB of 8-bit codes, pages of 64: 7.3 us; one load at a time, and teams of lanes joined by way of LDS, 9.7).
 // Pages of thousands of tokens leave a prompt few waves; a score of so many tokens says little, and the kernel is not made for them.
 #include <type_traits>
 

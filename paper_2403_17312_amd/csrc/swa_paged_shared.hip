@@ -381,13 +381,14 @@ __global__ void __launch_bounds__(256, Elem<C>::kBytes * D == 512 && ROWS == 2 ?
 // two tiles ahead, rows permuted by chunks instead of padded.  A wave stages eight tokens that follow each other, which lie in one page where page_size is a
 // multiple of eight: their place is a scalar.
 //
-// 64 sequences behind 32768 fp16 tokens, 64 query and 8 key heads: 101 us in all, its prefix 82 (0.84 PFLOP/s; the matrix cores are busy for a third of the clocks, the vector
-// units for another).  Measured and no faster: the halves in turns, one forming products while the other forms weights (102); more tiles' fragments ahead; three parts of the
-// tokens.
+// 64 sequences behind 32768 fp16 tokens, 64 query and 8 key heads: 137 us in all, without own tokens 127 (0.9 PFLOP/s with the products of the weights' second numbers; the matrix
+// cores are busy for a third of the clocks, the vector units for more than that).  Measured with weights of one number (101 us) and no faster: the halves in turns, one forming
+// products while the other forms weights (102); more tiles' fragments ahead; three parts of the tokens.
 //
 // Weights go to the second product as two numbers, as in the other forms, so that what a sequence gets does not hang on how many others its cache has room for: rounded once
 // they left outputs 1.3 to 1.4 times as far from 64 bits.  That is half as many products again.  Both are rounded to the nearest (split8), so an infinite value's product is
-// none; a unit with such a result is done again by the other form of the work.
+// none; a unit with such a result is done again by the other form of the work.  (us, one number / two: the above 103 / 137, 64 sequences behind 8192 bf16 tokens, 32 query heads
+// 38 / 41, 128 behind three of 2049 to 8191 with up to 1500 of their own 103 / 107.)
 
 // The 16 weights of one lane's column, exp2(c scale - m), their sum, and the rescaling that goes with them: formed with the reference m as it is, and again where that turns out
 // too low: in bf16 by a sum above 2^15 (or not finite, as on the first tile); in fp16, where the loudest weight is 2^15, by one that is no fp16 number.
@@ -706,7 +707,9 @@ __global__ void swa_paged_shared_alone_kernel(PagedRows rows, const int32_t* pre
 // Columns that a prefix can have.
 static int64_t most_columns(const swa_paged_params& p) { return (int64_t)(p.b - 1) * (p.h_q / p.h_kv); }
 
-// Columns of a prefix's unit, in sixteens.  More than 32 go to the wide form where it serves them.
+// Columns of a prefix's unit, in sixteens.  More than 32 go to the wide form where it serves them: us, units of 32 / wide, 32 query and 8 key heads of 128 channels, sequences with 16
+// to 300 tokens of their own: 10 behind 4096 23.0 / 24.8, 16 24.6 / 26.0, behind 32768 57.1 / 51.1, 24 behind 16000 44.5 / 42.2, 32 51.3 / 46.0, 64 behind 8192 45.8 / 41.0; 100 behind ten
+// of 500 to 2000 43.3 / 46.5; 64 channels, 32 behind 16000 35.6 / 35.6.
 static int shared_rows(const swa_paged_params& p)
 {
     const int64_t most = most_columns(p);
